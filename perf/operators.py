@@ -2,9 +2,9 @@
 gate and residual, the quantiser (with the SiLU gate or without) and the matrix product of 8-bit operands with a scale for
 each block of 128.
 
-8-bit values are e4m3 codes with fp32 scales.  Activations [R, C] have a scale per row and 128 columns, laid out
-[ceil(C / 128), R]; weights [N, K] one per 128 x 128, laid out [ceil(N / 128), ceil(K / 128)].  The scale of a block is its
-largest magnitude over 448, at least 2^-100.
+8-bit values are e4m3 codes with scales.  Activations [R, C] have a scale per row and 128 columns, laid out
+[ceil(C / 128), R]: the block's largest magnitude over 448, at least 2^-100, rounded to bf16.  Weights [N, K] have an fp32
+scale per 128 x 128, laid out [ceil(N / 128), ceil(K / 128)].
 
 A case is one call with what a program holds before it: activations, weights, norm parameters and, as a serving loop keeps
 them, the buffers that the results go to.  With ``own`` false the operators are computed from elementary torch operations in
@@ -83,7 +83,7 @@ def draw(rng):
     while True:
         M = _log(rng, 1, 8192)
         if op == "matmul":
-            c = _matmul(M, _width(rng, 100, 16384), _width(rng, 100, 16384), rng.choice(["bf16", "bf16", "f8", "f32"]))
+            c = _matmul(M, _width(rng, 100, 16384), _width(rng, 100, 16384), rng.choice(["bf16", "bf16", "f8"]))
             if c["M"] * c["K"] * c["N"] <= 4096 * 8192 * 16384 and c["K"] * c["N"] <= 8192 * 16384:
                 return c
             continue
@@ -103,26 +103,21 @@ def _expand(scales, width):
     return scales.t().repeat_interleave(BLOCK, 1)[:, :width]
 
 
-def _quantized(v):
-    """Codes and scales per row and 128 columns of v, in v's own precision up to the rounding of the codes."""
+def _coded(v):
+    """Codes and scales, per row and 128 columns, of fp32 v."""
     R, C = v.shape
     nb = -(-C // BLOCK)
     amax = torch.nn.functional.pad(v, (0, nb * BLOCK - C)).view(R, nb, BLOCK).abs().amax(2)
-    s = torch.clamp(amax / LARGEST, min=SMALLEST_SCALE).t().contiguous()
-    ratio = v / _expand(s, C)
-    return ratio, s
-
-
-def _coded(v):
-    ratio, s = _quantized(v)
-    return ratio.to(torch.float8_e4m3fn), s
+    s = torch.clamp(amax / LARGEST, min=SMALLEST_SCALE).t().contiguous().to(torch.bfloat16)
+    # a scale that was rounded down leaves at most 449.75, which rounds to 448
+    return (v / _expand(s.float(), C)).to(torch.float8_e4m3fn), s
 
 
 def _empty(out, M, d):
     """The buffer of a result: rows of codes are padded to 16 bytes."""
     if out == "f8":
         return (torch.empty(M, -(-d // 16) * 16, device="cuda", dtype=torch.float8_e4m3fn)[:, :d],
-                torch.empty(-(-d // BLOCK), M, device="cuda"))
+                torch.empty(-(-d // BLOCK), M, device="cuda", dtype=torch.bfloat16))
     return None if out == "none" else torch.empty(M, d, device="cuda", dtype=_DTYPES[out])
 
 
@@ -242,7 +237,8 @@ def run(state):
 
 
 def exact(case, seed):
-    """The same in 64 bits, from the operators' definitions.  8-bit results come as the values that the codes round."""
+    """The same in 64 bits, from the operators' definitions, before any result is rounded to its type: codes come as the values
+    that they round, v / scale, and scales before they go to bf16."""
     s = prepare(case, seed)
     got = []
     for v, out in _in_64_bits(s, case):
@@ -304,12 +300,12 @@ def work(case):
     M, op = case["M"], case["op"]
 
     def result(out, C):
-        return M * C + 4 * M * -(-C // BLOCK) if out == "f8" else M * C * size[out]
+        return M * C + 2 * M * -(-C // BLOCK) if out == "f8" else M * C * size[out]
 
     if op == "matmul":
         K, N = case["K"], case["N"]
         kb = -(-K // BLOCK)
-        return {"bytes": float(M * K + N * K + 4 * M * kb + 4 * -(-N // BLOCK) * kb + result(case["out"], N)), "flops": 2.0 * M * N * K}
+        return {"bytes": float(M * K + N * K + 2 * M * kb + 4 * -(-N // BLOCK) * kb + result(case["out"], N)), "flops": 2.0 * M * N * K}
     d, t = case["d"], size[case["type"]]
     if op == "quantize":
         return {"bytes": float(M * d * t * (2 if case["gated"] else 1) + result("f8", d)), "flops": (8.0 if case["gated"] else 3.0) * M * d}
