@@ -7,8 +7,9 @@ or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import struct
 from pathlib import Path
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -23,12 +24,18 @@ SVDMLP_SCRATCH_TOO_SMALL, SVDMLP_OUT_OF_HOST_MEMORY, SVDMLP_TIMED_OUT = -6, -7, 
 FLAG_FORCE_TILED, FLAG_FORCE_STREAM, FLAG_SKIP_ARCH_CHECK, FLAG_STREAM_ONE_KERNEL, FLAG_TILED_FUSED, FLAG_TILE_128 = 1, 2, 4, 8, 16, 32
 FLAG_PLAN_ROOM = 64
 FIRST_S1, FIRST_IN, OUT_256, OUT_128 = 1, 2, 1, 2
+SVDMLP_F8 = 2
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+GATE_PLAIN, GATE_SIGMOID, GATE_TANH = 0, 1, 2
+SCALE_BLOCK = 128
 
 EXPORTS = ["svdmlp_workspace_bytes", "svdmlp_create", "svdmlp_forward", "svdmlp_destroy", "svdmlp_status_string",
            "svdmlp_last_hip_error", "svdmlp_last_path", "svdmlp_abi_version", "svdmlp_profile_begin",
            "svdmlp_profile_end", "svdmlp_profile_kernel_name", "svdmlp_describe", "svdmlp_rank_for_ratio",
            "svdmlp_forward_static_scratch", "svdmlp_static_scratch_bytes",
-           "svdmlp_roof_read", "svdmlp_roof_mfma", "svdmlp_roof_mfma_operands", "svdmlp_roof_pingpong", "svdmlp_roof_empty", "svdmlp_roof_empty_chain", "svdmlp_force_plan", "svdmlp_roof_coexec", "svdmlp_check", "svdmlp_debug_set_poll_limit", "svdmlp_debug_preset_static_tickets"]
+           "svdmlp_roof_read", "svdmlp_roof_mfma", "svdmlp_roof_mfma_operands", "svdmlp_roof_pingpong", "svdmlp_roof_empty", "svdmlp_roof_empty_chain", "svdmlp_force_plan", "svdmlp_roof_coexec", "svdmlp_check", "svdmlp_debug_set_poll_limit", "svdmlp_debug_preset_static_tickets",
+           "svdmlp_quantize", "svdmlp_norm", "svdmlp_scaled_matmul", "svdmlp_scaled_matmul_workspace_bytes",
+           "svdmlp_scaled_matmul_describe"]
 
 
 class svdmlp_desc(ctypes.Structure):
@@ -41,6 +48,13 @@ class svdmlp_desc(ctypes.Structure):
         ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
         ("flags", ctypes.c_uint32),
     ]
+
+
+# The operators' argument structures of the header, field for field, as struct formats: a call packs its arguments into bytes
+# (1 us for the longest; filling a ctypes.Structure takes three times that, and the smallest calls are bound by it).
+QUANTIZE_ARGS = struct.Struct("=qqiiQQqqQQqq")
+NORM_ARGS = struct.Struct("=qqiiiiiiqffffQQqqQQQQqQQQqQqQq")
+SCALED_MATMUL_ARGS = struct.Struct("=qqqiiQQqqQQqQQqqQQ")
 
 
 class SvdMlpError(RuntimeError):
@@ -111,6 +125,15 @@ def lib() -> ctypes.CDLL:
         L.svdmlp_profile_kernel_name.restype = ctypes.c_char_p
         L.svdmlp_describe.argtypes = [ctypes.POINTER(svdmlp_desc), ctypes.c_int64, ctypes.c_char_p, ctypes.c_size_t]
         L.svdmlp_describe.restype = ctypes.c_int
+        # packed argument structures go as bytes
+        for name in ("svdmlp_quantize", "svdmlp_norm", "svdmlp_scaled_matmul"):
+            getattr(L, name).argtypes = [ctypes.c_char_p, ctypes.c_void_p]
+            getattr(L, name).restype = ctypes.c_int
+        L.svdmlp_scaled_matmul_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32]
+        L.svdmlp_scaled_matmul_workspace_bytes.restype = ctypes.c_size_t
+        L.svdmlp_scaled_matmul_describe.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_char_p,
+                                                    ctypes.c_size_t]
+        L.svdmlp_scaled_matmul_describe.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -322,3 +345,275 @@ class SvdMlp:
             self.close()
         except Exception:
             pass
+
+
+# ---- operators around a factored layer in 8 bits -----------------------------------------------------------------------
+class Scaled(NamedTuple):
+    """An 8-bit tensor: codes [R, C] (torch.float8_e4m3fn, rows starting on 16 bytes) times scales: activations bfloat16
+    [ceil(C / 128), R], one per row and 128 columns; weights float32 [ceil(R / 128), ceil(C / 128)], one per 128 x 128."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    def to_float(self) -> torch.Tensor:
+        """The values it stands for, in float32 (for looking at; the operators take the codes)."""
+        R, C = self.codes.shape
+        if self.scales.dtype == torch.bfloat16:
+            s = self.scales.t().float()
+        else:
+            s = self.scales.repeat_interleave(SCALE_BLOCK, 0)[:R]
+        return self.codes.float() * s.repeat_interleave(SCALE_BLOCK, 1)[:, :C]
+
+
+def empty_scaled(rows: int, cols: int, device, block_rows: int = 1) -> Scaled:
+    """An uninitialised 8-bit tensor, rows of codes padded to 16 bytes."""
+    blocks = -(-cols // SCALE_BLOCK)
+    codes = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+    if block_rows == 1:
+        return Scaled(codes, torch.empty((blocks, rows), dtype=torch.bfloat16, device=device))
+    return Scaled(codes, torch.empty((-(-rows // SCALE_BLOCK), blocks), dtype=torch.float32, device=device))
+
+
+_F8 = torch.float8_e4m3fn
+
+
+def _rows(t: torch.Tensor, what: str, shape, dtype, device, multiple: int = 1):
+    """(address, row stride) of a matrix on `device`: rows of consecutive elements, any stride between them."""
+    if not (t.dim() == 2 and t.shape == shape and t.dtype == dtype and t.device == device and (t.stride(1) == 1 or shape[1] == 1)):
+        raise ValueError(f"{what} must be a {tuple(shape)} {dtype} matrix on {device} whose rows lie in one piece, "
+                         f"got {tuple(t.shape)} {t.dtype} on {t.device} with strides {t.stride()}")
+    # the stride of a single row says nothing
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else (shape[1] + multiple - 1) // multiple * multiple
+
+
+def _vector(t: Optional[torch.Tensor], what: str, n: int, dtype, device) -> int:
+    if t is None:
+        return 0
+    if not (t.dim() == 1 and t.shape[0] == n and t.dtype == dtype and t.device == device and (t.stride(0) == 1 or n == 1)):
+        raise ValueError(f"{what} must be a contiguous {dtype} vector of {n} on {device}")
+    return t.data_ptr()
+
+
+def _codes(t, what: str, shape, device, weights: bool = False):
+    """(codes, codes stride, scales, scales stride)"""
+    codes, scales = t
+    ptr, ld = _rows(codes, what, shape, _F8, device, 16)
+    blocks = -(-shape[1] // SCALE_BLOCK)
+    if weights:
+        want = (-(-shape[0] // SCALE_BLOCK), blocks)
+        if not (scales.shape == want and scales.is_contiguous() and scales.dtype == torch.float32 and scales.device == device):
+            raise ValueError(f"the scales of {what} must be a contiguous float32 {want} on {device}")
+        return ptr, ld, scales.data_ptr(), blocks
+    sptr, sld = _rows(scales, f"the scales of {what}", (blocks, shape[0]), torch.bfloat16, device)
+    return ptr, ld, sptr, max(sld, shape[0])
+
+
+def _device_of(t: torch.Tensor, what: str):
+    if not (t.is_cuda and t.dim() == 2):
+        raise ValueError(f"{what} must be a matrix on the GPU")
+    return t.device
+
+
+def _run(name: str, rows: int, args: bytes, device, stream) -> None:
+    if rows == 0:            # a tensor of no rows has no address
+        return
+    s = _current_raw_stream(device.index) if stream is None else stream.cuda_stream
+    if device.index != torch.cuda.current_device():   # kernels are launched on the current device
+        with torch.cuda.device(device):
+            st = getattr(lib(), name)(args, s)
+    else:
+        st = getattr(lib(), name)(args, s)
+    if st != SVDMLP_OK:
+        raise SvdMlpError(st, name)
+
+
+def quantize(x: torch.Tensor, gate_with: Optional[torch.Tensor] = None, *, block_rows: int = 1, out=None,
+             stream: Optional[torch.cuda.Stream] = None) -> Scaled:
+    """x, or SiLU(x) * gate_with, as e4m3 codes with a scale per row and 128 columns (``block_rows=128``: weights, one per
+    128 x 128).  x: [R, C] bfloat16 or float32."""
+    dev = _device_of(x, "x")
+    if x.dtype not in _TORCH_DTYPE:
+        raise ValueError("x must be bfloat16 or float32")
+    R, C = x.shape
+    xp, xld = _rows(x, "x", x.shape, x.dtype, dev)
+    gp, gld = (0, 0) if gate_with is None else _rows(gate_with, "gate_with", x.shape, x.dtype, dev)
+    if out is None:
+        out = empty_scaled(R, C, dev, block_rows)
+    cp, cld, sp, sld = _codes(out, "out", x.shape, dev, block_rows != 1)
+    _run("svdmlp_quantize", R, QUANTIZE_ARGS.pack(R, C, _TORCH_DTYPE[x.dtype], block_rows, xp, gp, xld, gld, cp, sp, cld, sld), dev, stream)
+    return Scaled(*out)
+
+
+def _norm(branch, residual, weight, bias, kind, eps, weight_plus, residual_scale, branch_scale, gate, gate_rows, gate_act,
+          next_weight, next_bias, next_kind, next_eps, h, out, scaled, want_h, stream):
+    stream_t = residual if residual is not None else branch
+    dev = _device_of(stream_t, "x")
+    shape = stream_t.shape
+    M, d = shape
+    # the type of everything but the residual stream
+    of = next((t for t in (branch, weight, next_weight, bias, next_bias) if t is not None), None)
+    dtype = of.dtype if of is not None else stream_t.dtype
+    if dtype not in _TORCH_DTYPE or stream_t.dtype not in _TORCH_DTYPE:
+        raise ValueError("inputs must be bfloat16 or float32")
+    rp, rld = (0, 0) if residual is None else _rows(residual, "residual", shape, residual.dtype, dev)
+    bp, bld = (0, 0) if branch is None else _rows(branch, "branch", shape, dtype, dev)
+    gp = gld = 0
+    if gate is not None:
+        if gate_rows < 1:
+            raise ValueError("gate_rows must be at least 1")
+        gp, gld = _rows(gate, "gate", (-(-M // gate_rows), d), dtype, dev)
+    if h is None and want_h:
+        h = torch.empty((M, d), dtype=stream_t.dtype, device=dev)
+    hp, hld = (0, 0) if h is None else _rows(h, "h", shape, stream_t.dtype, dev)
+    op = old = sp = sld = 0
+    out_type = _TORCH_DTYPE[dtype]
+    if next_kind != NORM_NONE:
+        if out is None:
+            out = empty_scaled(M, d, dev) if scaled else torch.empty((M, d), dtype=dtype, device=dev)
+        if isinstance(out, tuple):
+            out_type = SVDMLP_F8
+            op, old, sp, sld = _codes(out, "out", shape, dev)
+            out = Scaled(*out)
+        else:
+            op, old = _rows(out, "out", shape, dtype, dev)
+    args = NORM_ARGS.pack(
+        M, d, _TORCH_DTYPE[dtype], _TORCH_DTYPE[stream_t.dtype], out_type, kind, next_kind, gate_act, gate_rows, eps, next_eps,
+        weight_plus, residual_scale, rp, bp, rld, bld, _vector(weight, "weight", d, dtype, dev), _vector(bias, "bias", d, dtype, dev),
+        _vector(branch_scale, "branch_scale", d, dtype, dev), gp, gld, _vector(next_weight, "next_weight", d, dtype, dev),
+        _vector(next_bias, "next_bias", d, dtype, dev), hp, hld, op, old, sp, sld)
+    _run("svdmlp_norm", M, args, dev, stream)
+    return h, out
+
+
+def norm_in(x: torch.Tensor, weight: Optional[torch.Tensor] = None, *, bias: Optional[torch.Tensor] = None,
+            add: Optional[torch.Tensor] = None, kind: int = NORM_RMS, eps: float = 1e-6, weight_plus: float = 0.0,
+            residual_scale: float = 1.0, h: Optional[torch.Tensor] = None, out=None, scaled: bool = False,
+            stream: Optional[torch.cuda.Stream] = None):
+    """The norm before a block: norm(residual_scale * x + add) * (weight + weight_plus) + bias, as a tensor of the weights'
+    type or, with ``scaled`` (or a ``Scaled`` as ``out``), in 8 bits.  x is the residual stream, float32 or of the weights'
+    type; ``add`` what the block before adds to it; the sum goes to ``h`` if that is given (x itself is allowed)."""
+    return _norm(add, x, None, None, NORM_NONE, eps, weight_plus, residual_scale, None, None, 1, GATE_PLAIN, weight, bias, kind,
+                 eps, h, out, scaled, False, stream)[1]
+
+
+def norm_out(branch: torch.Tensor, residual: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None, *,
+             bias: Optional[torch.Tensor] = None, kind: int = NORM_RMS, eps: float = 1e-6, weight_plus: float = 0.0,
+             residual_scale: float = 1.0, branch_scale: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+             gate_rows: int = 1, gate_act: int = GATE_PLAIN, next_weight: Optional[torch.Tensor] = None,
+             next_bias: Optional[torch.Tensor] = None, next_kind: Optional[int] = None, next_eps: Optional[float] = None,
+             h: Optional[torch.Tensor] = None, out=None, scaled: bool = False, stream: Optional[torch.cuda.Stream] = None):
+    """What follows a block: h = residual_scale * residual + [norm(branch) * (weight + weight_plus) + bias] * branch_scale *
+    act(gate[row // gate_rows]).  With a next norm (next_kind, or any of next_weight, next_bias, out and scaled) also the norm
+    before the next block, as ``norm_in`` makes it.  Returns (h, out or None); ``h`` may be ``residual``."""
+    if next_kind is None:
+        wanted = out is not None or scaled or next_weight is not None or next_bias is not None
+        next_kind = NORM_RMS if wanted else NORM_NONE
+    return _norm(branch, residual, weight, bias, kind, eps, weight_plus, residual_scale, branch_scale, gate, gate_rows, gate_act,
+                 next_weight, next_bias, next_kind, eps if next_eps is None else next_eps, h, out, scaled, True, stream)
+
+
+def svdmlp_scaled_matmul_workspace_bytes(M: int, N: int, K: int, out_type: int) -> int:
+    return int(lib().svdmlp_scaled_matmul_workspace_bytes(int(M), int(N), int(K), int(out_type)))
+
+
+def svdmlp_scaled_matmul_describe(M: int, N: int, K: int, out_type: int) -> str:
+    buf = ctypes.create_string_buffer(512)
+    _check(lib().svdmlp_scaled_matmul_describe(int(M), int(N), int(K), int(out_type), buf, len(buf)), "svdmlp_scaled_matmul_describe")
+    return buf.value.decode()
+
+
+def scaled_matmul(a, w, *, out=None, out_dtype: torch.dtype = torch.bfloat16, stream: Optional[torch.cuda.Stream] = None):
+    """a [M, K] times the transpose of w [N, K], both ``Scaled`` (or pairs of codes and scales): activations with a scale per
+    row and 128 columns, weights with one per 128 x 128.  The result [M, N] is ``out`` or a new tensor of ``out_dtype``;
+    torch.float8_e4m3fn (or a ``Scaled`` as ``out``) makes it the next product's activations."""
+    dev = _device_of(a[0], "a")
+    M, K = a[0].shape
+    if w[0].dim() != 2 or w[0].shape[1] != K:
+        raise ValueError(f"w must be [N, {K}]")
+    N = w[0].shape[0]
+    ap, ald, asp, asld = _codes(a, "a", (M, K), dev)
+    wp, wld, wsp, _ = _codes(w, "w", (N, K), dev, True)
+    if out is None:
+        if out_dtype not in (torch.bfloat16, _F8):
+            raise ValueError("out_dtype must be bfloat16 or float8_e4m3fn")
+        out = empty_scaled(M, N, dev) if out_dtype == _F8 else torch.empty((M, N), dtype=out_dtype, device=dev)
+    csp = csld = 0
+    if isinstance(out, tuple):
+        out_type = SVDMLP_F8
+        cp, cld, csp, csld = _codes(out, "out", (M, N), dev)
+        out = Scaled(*out)
+    else:
+        out_type = SVDMLP_BF16
+        cp, cld = _rows(out, "out", (M, N), torch.bfloat16, dev)
+    need = lib().svdmlp_scaled_matmul_workspace_bytes(M, N, K, out_type)
+    ws = None
+    if need:
+        if stream is None:
+            ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        else:                        # of the stream that uses it, so that it is not handed out again too early
+            with torch.cuda.stream(stream):
+                ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    _run("svdmlp_scaled_matmul", M, SCALED_MATMUL_ARGS.pack(M, N, K, out_type, 0, ap, asp, ald, asld, wp, wsp, wld, cp, csp, cld, csld,
+                                                         ws.data_ptr() if need else 0, need), dev, stream)
+    return out
+
+
+class SvdMlpF8:
+    """``SvdMlp`` in 8 bits: the factors are quantised once (a scale per 128 x 128), activations between the products carry a
+    scale per row and 128 columns, the result is bfloat16.  Arguments as ``SvdMlp``; no context, no limit on the row count."""
+
+    def __init__(self, *, Ug: torch.Tensor, Vg: torch.Tensor, Uu: Optional[torch.Tensor] = None, Vu: Optional[torch.Tensor] = None,
+                 Ud: Optional[torch.Tensor] = None, Vd: Optional[torch.Tensor] = None, kind: int = SVDMLP_GATED):
+        if kind not in (SVDMLP_GATED, SVDMLP_LINEAR):
+            raise ValueError("kind must be SVDMLP_GATED or SVDMLP_LINEAR")
+        if kind == SVDMLP_GATED and any(t is None for t in (Uu, Vu, Ud, Vd)):
+            raise ValueError("a gated block has six factors")
+        used = [Ug, Vg] if kind == SVDMLP_LINEAR else [Ug, Vg, Uu, Vu, Ud, Vd]
+        for t in used:
+            if not (t.is_cuda and t.dim() == 2 and t.dtype == Ug.dtype and t.device == Ug.device) or t.dtype not in _TORCH_DTYPE:
+                raise ValueError("factors must be device matrices of one dtype, bfloat16 or float32")
+        self.kind = kind
+        self.d, self.r = Ug.shape
+        self.ffn = Vg.shape[1]
+        self.r_down = Ud.shape[1] if kind == SVDMLP_GATED else 0
+        shapes = [(self.d, self.r), (self.r, self.ffn)] * (len(used) // 4 + 1)
+        shapes = shapes[:len(used)] if kind == SVDMLP_LINEAR else shapes[:4] + [(self.ffn, self.r_down), (self.r_down, self.d)]
+        if [tuple(t.shape) for t in used] != shapes:
+            raise ValueError(f"factor shapes {[tuple(t.shape) for t in used]} do not make a block, expected {shapes}")
+
+        def weights(*parts):
+            """Products take weights as [columns, contraction]; a rank ends on a block of 128, zero columns behind it."""
+            return quantize(torch.cat([p.t() for p in parts]), block_rows=SCALE_BLOCK)
+
+        def ranked(U):
+            return torch.nn.functional.pad(U, (0, -U.shape[1] % SCALE_BLOCK))
+
+        def rank_rows(V):
+            return torch.nn.functional.pad(V, (0, 0, 0, -V.shape[0] % SCALE_BLOCK))
+
+        if kind == SVDMLP_LINEAR:
+            self.first, self.last = weights(ranked(Ug)), weights(rank_rows(Vg))
+        else:
+            self.first = weights(ranked(Ug), ranked(Uu))
+            self.gate, self.up = weights(rank_rows(Vg)), weights(rank_rows(Vu))
+            self.down, self.last = weights(ranked(Ud)), weights(rank_rows(Vd))
+
+    def out_features(self) -> int:
+        return self.d if self.kind == SVDMLP_GATED else self.ffn
+
+    def forward(self, X, out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """X: [M, d] bfloat16 or float32, or ``Scaled`` as ``norm_in`` makes it.  The result is ``out`` or a new tensor."""
+        if stream is not None:       # everything in between belongs to that stream
+            with torch.cuda.stream(stream):
+                return self.forward(X, out)
+        if not isinstance(X, tuple):
+            X = quantize(X)
+        T = scaled_matmul(X, self.first, out_dtype=_F8)
+        if self.kind == SVDMLP_GATED:
+            rank = self.gate.codes.shape[1]
+            blocks = rank // SCALE_BLOCK
+            G = scaled_matmul(Scaled(T.codes[:, :rank], T.scales[:blocks]), self.gate)
+            P = scaled_matmul(Scaled(T.codes[:, rank:], T.scales[blocks:]), self.up)
+            T = scaled_matmul(quantize(G, P), self.down, out_dtype=_F8)
+        return scaled_matmul(T, self.last, out=out)
+
+    __call__ = forward

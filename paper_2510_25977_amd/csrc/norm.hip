@@ -1,0 +1,213 @@
+// The norms around a block of the residual stream, with the residual, the gate and the scales, in one pass:
+//   b = [norm(branch) (weight + plus) + bias] branch_scale act(gate)    h = residual_scale residual + b    out = norm(h) ..
+// A row lies in the registers of its threads in fp32 from its first load to its last store, so every input is read once and
+// every result written once; two or three bytes move per instruction and element, so HBM bounds it.
+#include "scaled.h"
+
+namespace svdmlp {
+
+struct NormP {
+  const void *residual, *branch, *weight, *bias, *branch_scale, *gate, *next_weight, *next_bias;
+  void *h, *out;
+  __bf16* out_scales;
+  int64_t residual_ld, branch_ld, gate_ld, h_ld, out_ld, out_scales_ld, gate_rows;
+  int64_t rows;
+  int d, kind, next_kind, gate_act, out_f8;
+  float eps, next_eps, weight_plus, residual_scale, inv_d;
+};
+
+// Sum over the TPR threads of a row.  part: one float per wave, a buffer of its own for every call of a kernel.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float x, float* part) {
+  x = sum64(x);
+  if constexpr (TPR > 64) {
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = 0.f;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; ++w) x += part[w];
+  }
+  return x;
+}
+
+// v <- its norm, without weight.  Columns beyond d hold zeros and are left out of the second sum of a LAYER norm.
+template <int TPR, int NV>
+__device__ __forceinline__ void normalize(float (&v)[NV][8], int kind, float eps, const NormP& p, int t, float* part) {
+  if (kind == SVDMLP_NORM_LAYER) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += v[i][e];
+    const float mean = row_sum<TPR>(s, part) * p.inv_d;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = (i * TPR + t) * 8 + e < p.d ? v[i][e] - mean : 0.f;
+    part += TPR / 64;
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += v[i][e] * v[i][e];
+  const float scale = 1.f / sqrtf(row_sum<TPR>(s, part) * p.inv_d + eps);
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[i][e] *= scale;
+}
+
+template <class T>
+__device__ __forceinline__ void affine(float (&x)[8], const void* weight, const void* bias, int col, const NormP& p) {
+  if (weight) {
+    const Raw8<T> w = load8((const T*)weight, col, p.d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= w.get(e) + p.weight_plus;
+  }
+  if (bias) {
+    const Raw8<T> b = load8((const T*)bias, col, p.d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] += b.get(e);
+  }
+}
+
+// TPR threads hold a row, thread t columns 8 (i TPR + t) .. + 7, i < NV: 16 lanes hold a block of 128 columns.
+template <class T, class S, int TPR, int NV>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormP p) {
+  constexpr int WAVES = TPR / 64;
+  __shared__ float part[4 * WAVES];
+  const int t = threadIdx.x % TPR;
+  const int64_t row = (int64_t)blockIdx.x * (TPR < 256 ? 256 / TPR : 1) + threadIdx.x / TPR;
+  if (row >= p.rows) return;   // whole waves, and whole workgroups where they meet at a barrier
+  Raw8<T> rb[NV];
+  Raw8<S> rr[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int col = (i * TPR + t) * 8;
+    rb[i] = p.branch && col < p.d ? load8((const T*)p.branch + row * p.branch_ld, col, p.d) : Raw8<T>{};
+    rr[i] = p.residual && col < p.d ? load8((const S*)p.residual + row * p.residual_ld, col, p.d) : Raw8<S>{};
+  }
+  float v[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[i][e] = rb[i].get(e);
+  if (p.kind != SVDMLP_NORM_NONE) normalize<TPR, NV>(v, p.kind, p.eps, p, t, part);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int col = (i * TPR + t) * 8;
+    if (col >= p.d) continue;
+    if (p.kind != SVDMLP_NORM_NONE) affine<T>(v[i], p.weight, p.bias, col, p);
+    if (p.branch_scale) {
+      const Raw8<T> s = load8((const T*)p.branch_scale, col, p.d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] *= s.get(e);
+    }
+    if (p.gate) {
+      const Raw8<T> s = load8((const T*)p.gate + row / p.gate_rows * p.gate_ld, col, p.d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float g = s.get(e);
+        v[i][e] *= p.gate_act == SVDMLP_GATE_SIGMOID ? 1.f / (1.f + __expf(-g)) : p.gate_act == SVDMLP_GATE_TANH ? tanhf(g) : g;
+      }
+    }
+    if (p.residual) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] += p.residual_scale * rr[i].get(e);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (col + e >= p.d) v[i][e] = 0.f;
+    if (p.h) store8((S*)p.h + row * p.h_ld, col, p.d, v[i]);
+  }
+  if (p.next_kind == SVDMLP_NORM_NONE) return;
+  normalize<TPR, NV>(v, p.next_kind, p.next_eps, p, t, part + 2 * WAVES);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int col = (i * TPR + t) * 8;
+    if (col < p.d) affine<T>(v[i], p.next_weight, p.next_bias, col, p);
+    if (!p.out_f8) {
+      if (col < p.d) store8((T*)p.out + row * p.out_ld, col, p.d, v[i]);
+      continue;
+    }
+    float amax = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (col + e >= p.d) v[i][e] = 0.f;
+      amax = fmaxf(amax, fabsf(v[i][e]));
+    }
+    const __bf16 s = scale_of(max16(amax));
+    if (col < p.d) {
+      store_codes8((unsigned char*)p.out + row * p.out_ld, col, p.d, v[i], 1.f / (float)s);
+      if (t % 16 == 0) p.out_scales[(int64_t)(col / SCALE_BLOCK) * p.out_scales_ld + row] = s;
+    }
+  }
+}
+
+template <class T, class S, int TPR, int NV>
+static void run_norm(const NormP& p, hipStream_t st) {
+  constexpr int per = TPR < 256 ? 256 / TPR : 1;
+  k_norm<T, S, TPR, NV><<<(unsigned)((p.rows + per - 1) / per), TPR < 256 ? 256 : TPR, 0, st>>>(p);
+}
+
+template <class T, class S>
+static void launch_norm(const NormP& p, hipStream_t st) {
+  if (p.d <= 512) run_norm<T, S, 64, 1>(p, st);
+  else if (p.d <= 2048) run_norm<T, S, 256, 1>(p, st);
+  else if (p.d <= 4096) run_norm<T, S, 256, 2>(p, st);
+  else if (p.d <= 8192) run_norm<T, S, 256, 4>(p, st);
+  else run_norm<T, S, 1024, 4>(p, st);
+}
+
+static bool known_norm(int k) { return k == SVDMLP_NORM_NONE || k == SVDMLP_NORM_RMS || k == SVDMLP_NORM_LAYER; }
+
+}  // namespace svdmlp
+
+using namespace svdmlp;
+
+extern "C" int svdmlp_norm(const svdmlp_norm_args* a, void* hip_stream) {
+  if (!a || a->rows < 0 || a->d <= 0 || !is_float_type(a->type) || !is_float_type(a->stream_type)) return SVDMLP_INVALID_ARGUMENT;
+  if (a->out_type != a->type && a->out_type != SVDMLP_F8) return SVDMLP_INVALID_ARGUMENT;
+  if (!known_norm(a->kind) || !known_norm(a->next_kind)) return SVDMLP_INVALID_ARGUMENT;
+  if (a->gate_act < SVDMLP_GATE_PLAIN || a->gate_act > SVDMLP_GATE_TANH) return SVDMLP_INVALID_ARGUMENT;
+  if (!a->residual && !a->branch) return SVDMLP_INVALID_ARGUMENT;
+  const bool next = a->next_kind != SVDMLP_NORM_NONE;
+  if (next != (a->out != nullptr) || (!next && !a->h)) return SVDMLP_INVALID_ARGUMENT;
+  if (!a->branch && (a->kind != SVDMLP_NORM_NONE || a->branch_scale || a->gate)) return SVDMLP_INVALID_ARGUMENT;
+  if ((a->kind != SVDMLP_NORM_NONE && !(a->eps > 0.f)) || (next && !(a->next_eps > 0.f))) return SVDMLP_INVALID_ARGUMENT;
+  if ((a->kind == SVDMLP_NORM_NONE && (a->weight || a->bias)) || (!next && (a->next_weight || a->next_bias))) return SVDMLP_INVALID_ARGUMENT;
+  if (a->gate && (a->gate_rows < 1 || a->gate_ld < a->d)) return SVDMLP_INVALID_ARGUMENT;
+  if ((a->residual && a->residual_ld < a->d) || (a->branch && a->branch_ld < a->d) || (a->h && a->h_ld < a->d)) return SVDMLP_INVALID_ARGUMENT;
+  const size_t t = (size_t)type_bytes(a->type), s = (size_t)type_bytes(a->stream_type);
+  for (const void* q : {a->branch, a->weight, a->bias, a->branch_scale, a->gate, a->next_weight, a->next_bias})
+    if (!aligned_to(q, t)) return SVDMLP_INVALID_ARGUMENT;
+  if (!aligned_to(a->residual, s) || !aligned_to(a->h, s)) return SVDMLP_INVALID_ARGUMENT;
+  if (next && a->out_type == SVDMLP_F8) {
+    if (const int st = check_codes(a->out, a->out_ld, a->d)) return st;
+    if (!a->out_scales || !aligned_to(a->out_scales, 2) || a->out_scales_ld < a->rows) return SVDMLP_INVALID_ARGUMENT;
+  } else if (next && (a->out_ld < a->d || !aligned_to(a->out, t))) {
+    return SVDMLP_INVALID_ARGUMENT;
+  }
+  // h may take the place of the residual, element for element; nothing else may share a buffer
+  if (a->h && a->h == a->residual && a->h_ld != a->residual_ld) return SVDMLP_INVALID_ARGUMENT;
+  if ((a->h && (a->h == a->branch || a->h == a->out)) || (a->out && (a->out == a->residual || a->out == a->branch))) return SVDMLP_INVALID_ARGUMENT;
+  if (a->type == SVDMLP_F32 && a->stream_type == SVDMLP_BF16) return SVDMLP_UNSUPPORTED;
+  if (a->d > 32768 || a->rows >= int64_t(1) << 21) return SVDMLP_UNSUPPORTED;   // registers of a workgroup; a grid below 2^31 lanes
+  if (a->rows == 0) return SVDMLP_OK;
+  NormP p;
+  p.residual = a->residual; p.branch = a->branch; p.weight = a->weight; p.bias = a->bias;
+  p.branch_scale = a->branch_scale; p.gate = a->gate; p.next_weight = a->next_weight; p.next_bias = a->next_bias;
+  p.h = a->h; p.out = a->out; p.out_scales = (__bf16*)a->out_scales;
+  p.residual_ld = a->residual_ld; p.branch_ld = a->branch_ld; p.gate_ld = a->gate_ld; p.h_ld = a->h_ld; p.out_ld = a->out_ld;
+  p.out_scales_ld = a->out_scales_ld; p.gate_rows = a->gate_rows < 1 ? 1 : a->gate_rows;
+  p.rows = a->rows; p.d = (int)a->d; p.kind = a->kind; p.next_kind = a->next_kind; p.gate_act = a->gate_act;
+  p.out_f8 = next && a->out_type == SVDMLP_F8;
+  p.eps = a->eps; p.next_eps = a->next_eps; p.weight_plus = a->weight_plus; p.residual_scale = a->residual_scale;
+  p.inv_d = (float)(1.0 / (double)a->d);
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (a->type == SVDMLP_F32) launch_norm<float, float>(p, st);
+  else if (a->stream_type == SVDMLP_F32) launch_norm<__bf16, float>(p, st);
+  else launch_norm<__bf16, __bf16>(p, st);
+  return launch_status();
+}

@@ -1,0 +1,204 @@
+"""Host-only checks of the 8-bit operators: what they refuse, before anything touches a device, and the 64-bit oracle."""
+import ctypes
+import re
+import types
+
+import numpy as np
+import pytest
+import torch
+
+import oracle.scaled as ref
+from paper_2510_25977_amd import binding as B
+from tests.conftest import ROOT
+
+OK, BAD, UNSUPPORTED, SMALL = B.SVDMLP_OK, B.SVDMLP_INVALID_ARGUMENT, B.SVDMLP_UNSUPPORTED, B.SVDMLP_WORKSPACE_TOO_SMALL
+BF16, F32, F8 = B.SVDMLP_BF16, B.SVDMLP_F32, B.SVDMLP_F8
+
+# the fields of the header's argument structures with a call that is right in everything but that it has no rows
+QUANTIZE = dict(rows=0, cols=256, type=BF16, block_rows=1, x=0x1000, gated=0, x_ld=256, gated_ld=0, codes=0x2000, scales=0x3000,
+                codes_ld=256, scales_ld=64)
+NORM = dict(rows=0, d=256, type=BF16, stream_type=BF16, out_type=F8, kind=B.NORM_RMS, next_kind=B.NORM_RMS, gate_act=0, gate_rows=4,
+            eps=1e-6, next_eps=1e-6, weight_plus=0.0, residual_scale=1.0, residual=0x1000, branch=0x2000, residual_ld=256,
+            branch_ld=256, weight=0x3000, bias=0x3000, branch_scale=0x3000, gate=0x4000, gate_ld=256, next_weight=0x3000,
+            next_bias=0x3000, h=0x5000, h_ld=256, out=0x6000, out_ld=256, out_scales=0x7000, out_scales_ld=64)
+MATMUL = dict(M=0, N=64, K=256, out_type=F8, reserved=0, a=0x1000, a_scales=0x2000, a_ld=256, a_scales_ld=64, w=0x3000, w_scales=0x4000,
+              w_ld=256, c=0x5000, c_scales=0x6000, c_ld=64, c_scales_ld=64, workspace=0x7000, workspace_bytes=1 << 30)
+CALLS = {"svdmlp_quantize": (QUANTIZE, B.QUANTIZE_ARGS), "svdmlp_norm": (NORM, B.NORM_ARGS),
+         "svdmlp_scaled_matmul": (MATMUL, B.SCALED_MATMUL_ARGS)}
+
+
+def status(name, **changed):
+    fields, layout = CALLS[name]
+    assert set(changed) <= set(fields)
+    return getattr(B.lib(), name)(layout.pack(*{**fields, **changed}.values()), None)
+
+
+def test_packed_arguments_are_the_headers_structures():
+    """The struct formats of the binding field for field against the header: order, kind and size."""
+    text = re.sub(r"/\*.*?\*/", "", (ROOT / "include" / "svdmlp.h").read_text(), flags=re.S)
+    for name, (fields, layout) in CALLS.items():
+        body = re.search(r"typedef struct \{([^}]*)\}\s*" + name + "_args;", text).group(1)
+        names, fmt = [], ""
+        for line in body.split(";"):
+            if not line.strip():
+                continue
+            kind, rest = re.match(r"\s*(const void|void|const float|float|int64_t|int32_t|size_t)\b(.*)", line, flags=re.S).groups()
+            for f in rest.split(","):
+                fmt += "Q" if "*" in f or kind == "size_t" else {"int64_t": "q", "int32_t": "i", "float": "f"}[kind]
+                names.append(f.strip(" *\n"))
+        assert names == list(fields), name
+        assert "=" + fmt == layout.format, name
+        native = ctypes.sizeof(type("S", (ctypes.Structure,), {"_fields_": [
+            (f"f{i}", {"q": ctypes.c_int64, "i": ctypes.c_int32, "f": ctypes.c_float, "Q": ctypes.c_void_p}[c]) for i, c in enumerate(fmt)]}))
+        assert native == layout.size, name                 # the C layout has no gaps
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_no_rows_are_accepted_and_null_arguments_refused(name):
+    assert status(name) == OK
+    assert getattr(B.lib(), name)(None, None) == BAD
+
+
+@pytest.mark.parametrize("changed,want", [
+    (dict(rows=-1), BAD), (dict(cols=0), BAD), (dict(type=F8), BAD), (dict(type=7), BAD), (dict(block_rows=64), BAD),
+    (dict(x=0), BAD), (dict(x=0x1001), BAD), (dict(x_ld=255), BAD), (dict(gated=0x1001, gated_ld=256), BAD), (dict(gated=0x1100, gated_ld=10), BAD),
+    (dict(codes=0), BAD), (dict(codes=0x2008), BAD), (dict(codes_ld=264), BAD), (dict(codes_ld=240), BAD), (dict(scales=0), BAD),
+    (dict(scales=0x3001), BAD), (dict(block_rows=128, scales=0x3002), BAD), (dict(codes=0x1000), BAD), (dict(rows=65), BAD), (dict(codes_ld=1 << 23), UNSUPPORTED),
+    (dict(block_rows=128, gated=0x1100, gated_ld=256), BAD), (dict(rows=1 << 24, scales_ld=1 << 24), UNSUPPORTED),
+    (dict(cols=1 << 23, x_ld=1 << 23, codes_ld=(1 << 23) - 16), BAD), (dict(block_rows=128, scales_ld=0), OK), (dict(gated=0x1100, gated_ld=300), OK),
+])
+def test_quantize_refuses(changed, want):
+    assert status("svdmlp_quantize", **changed) == want
+
+
+@pytest.mark.parametrize("changed,want", [
+    (dict(rows=-1), BAD), (dict(d=0), BAD), (dict(type=F8), BAD), (dict(stream_type=5), BAD), (dict(out_type=F32), BAD),
+    (dict(kind=3), BAD), (dict(next_kind=-1), BAD), (dict(gate_act=3), BAD), (dict(residual=0, branch=0), BAD), (dict(out=0), BAD),
+    (dict(next_kind=B.NORM_NONE), BAD),                                             # an out that nothing makes
+    (dict(next_kind=B.NORM_NONE, out=0, h=0), BAD), (dict(next_kind=B.NORM_NONE, out=0), BAD),      # next_weight without a norm
+    (dict(next_kind=B.NORM_NONE, out=0, next_weight=0, next_bias=0), OK),
+    (dict(branch=0), BAD), (dict(kind=B.NORM_NONE), BAD), (dict(kind=B.NORM_NONE, weight=0, bias=0), OK), (dict(eps=0.0), BAD),
+    (dict(eps=float("nan")), BAD), (dict(next_eps=-1.0), BAD), (dict(gate_rows=0), BAD), (dict(gate_ld=255), BAD), (dict(gate=0, gate_rows=0), OK),
+    (dict(residual_ld=255), BAD), (dict(branch_ld=10), BAD), (dict(h_ld=255), BAD), (dict(weight=0x3001), BAD), (dict(h=0x5001), BAD),
+    (dict(stream_type=F32, residual=0x1002), BAD), (dict(out=0x6008), BAD), (dict(out_ld=264), BAD), (dict(out_scales=0), BAD),
+    (dict(rows=65), BAD), (dict(out_type=BF16, out_ld=255), BAD), (dict(out_type=BF16, out=0x6001), BAD), (dict(out_type=BF16, out_scales=0), OK),
+    (dict(h=0x1000), OK), (dict(h=0x1000, h_ld=300), BAD), (dict(h=0x2000), BAD), (dict(out=0x1000), BAD), (dict(out=0x5000), BAD),
+    (dict(type=F32, stream_type=BF16, out_type=F32), UNSUPPORTED), (dict(stream_type=F32), OK), (dict(residual=0), OK), (dict(h=0), OK),
+    (dict(d=32769, residual_ld=40000, branch_ld=40000, gate_ld=40000, h_ld=40000, out_ld=40000), UNSUPPORTED),
+    (dict(rows=1 << 21, out_scales_ld=1 << 21), UNSUPPORTED),
+])
+def test_norm_refuses(changed, want):
+    assert status("svdmlp_norm", **changed) == want
+
+
+@pytest.mark.parametrize("changed,want", [
+    (dict(M=-1), BAD), (dict(N=0), BAD), (dict(K=0), BAD), (dict(out_type=3), BAD), (dict(out_type=F32), BAD), (dict(reserved=1), BAD), (dict(a=0), BAD),
+    (dict(a=0x1008), BAD), (dict(a_ld=248), BAD), (dict(a_ld=240), BAD), (dict(w=0), BAD), (dict(w=0x3001), BAD), (dict(w_ld=255), BAD),
+    (dict(a_scales=0), BAD), (dict(w_scales=0), BAD), (dict(a_scales=0x2001), BAD), (dict(M=65), BAD), (dict(c=0), BAD), (dict(c=0x5004), BAD),
+    (dict(c_ld=56), BAD), (dict(c_scales=0), BAD), (dict(c=0x1000), BAD), (dict(c=0x3000), BAD), (dict(out_type=BF16, c=0x5001), BAD),
+    (dict(out_type=BF16, c=0x5002, c_ld=65), OK), (dict(out_type=BF16, c_ld=63), BAD), (dict(out_type=BF16, c_scales=0), OK),
+    (dict(a_ld=1 << 23), UNSUPPORTED), (dict(w_ld=1 << 23), UNSUPPORTED), (dict(M=1 << 24), UNSUPPORTED), (dict(N=(1 << 22) + 1), UNSUPPORTED),
+    (dict(K=(1 << 22) + 1), UNSUPPORTED),
+])
+def test_scaled_matmul_refuses(changed, want):
+    assert status("svdmlp_scaled_matmul", **changed) == want
+
+
+def test_scaled_matmul_workspace():
+    """Extents that need a workspace say so, and a call without it is refused; bad extents need none."""
+    need = B.svdmlp_scaled_matmul_workspace_bytes(16, 512, 14336, F8)
+    assert need >= 16 * 512 * 4
+    args = dict(M=16, N=512, K=14336, a_ld=14336, w_ld=14336, c_ld=512)
+    assert status("svdmlp_scaled_matmul", **args, workspace_bytes=need - 1) == SMALL
+    assert status("svdmlp_scaled_matmul", **args, workspace=0) == BAD
+    assert status("svdmlp_scaled_matmul", **args, workspace=0x7008) == BAD
+    for bad in ((-1, 1, 1, F8), (1, 0, 1, F8), (1, 1, 0, BF16), (1, 1, 1, F32)):
+        assert B.svdmlp_scaled_matmul_workspace_bytes(*bad) == 0
+        with pytest.raises(B.SvdMlpError):
+            B.svdmlp_scaled_matmul_describe(*bad)
+
+
+class _OnDevice(torch.Tensor):
+    """A CPU tensor that says it lies on the GPU: the binding's checks need no more."""
+    is_cuda = property(lambda self: True)
+
+
+def fake(*shape, dtype=torch.bfloat16):
+    return torch.zeros(*shape).to(dtype).as_subclass(_OnDevice)
+
+
+def test_the_binding_checks_tensors(monkeypatch):
+    monkeypatch.setattr(B, "_run", lambda *a: None)
+    x = fake(4, 256)
+    good = B.empty_scaled(4, 256, "cpu")
+    weights = B.empty_scaled(64, 256, "cpu", 128)
+    pair = (good.codes.as_subclass(_OnDevice), good.scales)
+    assert good.codes.shape == (4, 256) and good.scales.shape == (2, 4) and weights.scales.shape == (1, 2)
+    assert B.empty_scaled(3, 33, "cpu").codes.stride() == (48, 1)
+    assert B.quantize(x, out=good).codes is good.codes
+    for call in (lambda: B.quantize(torch.zeros(4, 256)),                                     # not on the GPU
+                 lambda: B.quantize(fake(4, 256, dtype=torch.float16)), lambda: B.quantize(fake(4, 4, 4)),
+                 lambda: B.quantize(x.t()),                                                   # columns in one piece, not rows
+                 lambda: B.quantize(x, fake(4, 255)), lambda: B.quantize(x, fake(4, 256, dtype=torch.float32)),
+                 lambda: B.quantize(x, out=B.empty_scaled(4, 255, "cpu")), lambda: B.quantize(x, out=weights),
+                 lambda: B.quantize(x, block_rows=128, out=(weights.codes[:4], good.scales)),
+                 lambda: B.norm_in(x, fake(255)), lambda: B.norm_in(x, fake(256, dtype=torch.float16)),
+                 lambda: B.norm_in(x, add=fake(5, 256)), lambda: B.norm_in(x, h=fake(4, 256, dtype=torch.float32)),
+                 lambda: B.norm_in(x, out=fake(4, 256, dtype=torch.float32)), lambda: B.norm_out(x, x, gate=fake(3, 256)),
+                 lambda: B.norm_out(x, x, gate=x, gate_rows=0), lambda: B.norm_out(x, x, gate=x, gate_rows=2),
+                 lambda: B.scaled_matmul(pair, B.empty_scaled(64, 128, "cpu", 128)),
+                 lambda: B.scaled_matmul(pair, (weights.codes, weights.scales.t())),
+                 lambda: B.scaled_matmul(pair, weights, out_dtype=torch.float32),
+                 lambda: B.scaled_matmul(pair, weights, out=fake(4, 64, dtype=torch.float32)),
+                 lambda: B.scaled_matmul(pair, weights, out=fake(4, 63)),
+                 lambda: B.scaled_matmul((x, good.scales), weights)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(ValueError):
+        B.SvdMlpF8(Ug=fake(256, 64), Vg=fake(64, 512))                                        # four factors missing
+    with pytest.raises(ValueError):
+        B.SvdMlpF8(Ug=fake(256, 64), Vg=fake(65, 512), kind=B.SVDMLP_LINEAR)
+
+
+def test_a_call_on_another_device_makes_it_current(monkeypatch):
+    """Kernels go to the current device, so an operator whose tensors lie elsewhere switches to theirs and back, and asks for
+    the current stream of that device."""
+    now, seen = [0], []
+
+    class on:
+        def __init__(self, device):
+            self.index = device.index
+
+        def __enter__(self):
+            self.before, now[0] = now[0], self.index
+
+        def __exit__(self, *e):
+            now[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", on)
+    monkeypatch.setattr(B, "_current_raw_stream", lambda index: 100 + index)
+    monkeypatch.setattr(B, "lib", lambda: types.SimpleNamespace(op=lambda args, stream: seen.append((now[0], stream)) or 0))
+    B._run("op", 1, b"", torch.device("cuda", 1), None)
+    B._run("op", 1, b"", torch.device("cuda", 0), None)
+    B._run("op", 1, b"", torch.device("cuda", 1), types.SimpleNamespace(cuda_stream=7))
+    assert seen == [(1, 101), (0, 100), (1, 7)] and now == [0]
+
+
+def test_the_e4m3_table_of_the_oracle():
+    codes = torch.arange(256, dtype=torch.int32).to(torch.uint8)
+    want = codes.view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(ref.E4M3, want, equal_nan=True)
+    assert np.nanmax(ref.E4M3) == ref.LARGEST and np.isnan(ref.E4M3).sum() == 2
+
+
+def test_the_oracles_scales_on_a_case_by_hand():
+    v = np.zeros((3, 130))
+    v[0, 0], v[0, 129], v[1, 5], v[2, 128] = 448.0, -896.0, 44.8, 1e-40
+    s = ref.scales_of(v)
+    assert s.shape == (2, 3)
+    assert np.allclose(s, [[1.0, 0.1, 2.0 ** -100], [2.0, 2.0 ** -100, 2.0 ** -100]], rtol=1e-15)
+    assert np.allclose(ref.scales_of(v, 128), [[1.0, 2.0]], rtol=1e-15)
+    codes = np.full((3, 130), 0x38, np.uint8)                                       # 1.0
+    assert np.allclose(ref.activations(codes, s)[:, [0, 127, 128]], s.T[:, [0, 0, 1]])
+    assert np.allclose(ref.weights(codes, np.array([[1.0, 2.0]]))[1, [127, 129]], [1.0, 2.0])
