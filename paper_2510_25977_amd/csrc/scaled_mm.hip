@@ -58,94 +58,181 @@ __device__ __forceinline__ i32x8 block_codes(const char* row, int b, int g, int 
   return join16(codes16_to(row, c, K), codes16_to(row, c + 64, K));
 }
 
-__device__ __forceinline__ void store4(const MmP& p, int m, int n, const f32x4& v) {
-  if (m >= p.M || n >= p.N) return;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (n + e >= p.N) return;
-    ((__bf16*)p.c)[m * p.c_ld + n + e] = (__bf16)v[e];
-  }
-}
-
-// Few rows, up to 16 MT: the weights go from HBM straight into registers, once.  A workgroup has 16 NT columns and a range
-// of the contraction, whose blocks go to its waves in turn; the waves' sums meet in LDS.
-template <int MT, int NT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void k_mm_few(MmP p) {
-  __shared__ f32x4 red[WAVES][MT * NT][64];
+// ---- up to 16 rows ------------------------------------------------------------------------------------
+// The weights go from HBM straight into registers, once.  A workgroup has 16 columns and a range of the contraction, whose
+// blocks go to its eight waves in turn, four at a time, all loads before the first product; the waves' sums meet in LDS.  One
+// row by W[4096, 4096] takes 6.1 us in a graph, by W[8192, 4096] 8.5 us (5.6 TB/s without the 2.5 us of a launch with one
+// load in it); two column tiles a workgroup 7.6 and 8.4 us, sixteen waves 6.3 and 8.5 us.
+constexpr int FEW_WAVES = 8;
+__global__ __launch_bounds__(64 * FEW_WAVES) void k_mm_few(MmP p) {
+  __shared__ f32x4 red[FEW_WAVES][64];
   const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int ntiles = (p.N + 16 * NT - 1) / (16 * NT), z = blockIdx.x / ntiles;
-  const int n0 = (blockIdx.x - z * ntiles) * 16 * NT;
-  const char *wr[NT], *ar[MT];
-  const __bf16* sa[MT];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) wr[j] = p.w + (int64_t)min(n0 + 16 * j + r, p.N - 1) * p.w_ld;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int m = min(16 * i + r, p.M - 1);
-    ar[i] = p.a + m * p.a_ld;
-    sa[i] = p.sa + m;
-  }
+  const int ntiles = (p.N + 15) / 16, z = blockIdx.x / ntiles, n0 = (blockIdx.x - z * ntiles) * 16;
+  const char* wr = p.w + (int64_t)min(n0 + r, p.N - 1) * p.w_ld;
+  const char* ar = p.a + min(r, p.M - 1) * p.a_ld;
+  const __bf16* sa = p.sa + min(r, p.M - 1);
   const float* sw = p.sw + (int64_t)(n0 / SCALE_BLOCK) * p.KB;
-  f32x4 acc[NT][MT] = {};
-  // U blocks of this wave from b on, all loads before the first product
+  f32x4 acc = {};
+  // U blocks of this wave from b on
   auto blocks = [&](auto full, auto u, int b) {
     constexpr bool FULL = decltype(full)::value;
     constexpr int U = decltype(u)::value;
-    i32x8 fw[U][NT], fa[U][MT];
-    float s[U][MT];
+    i32x8 fw[U], fa[U];
+    float s[U];
 #pragma unroll
     for (int x = 0; x < U; ++x) {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) fw[x][j] = block_codes<FULL>(wr[j], b + x * WAVES, g, p.K);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        fa[x][i] = block_codes<FULL>(ar[i], b + x * WAVES, g, p.K);
-        s[x][i] = (float)sa[i][(b + x * WAVES) * p.sa_ld] * sw[b + x * WAVES];
-      }
+      fw[x] = block_codes<FULL>(wr, b + x * FEW_WAVES, g, p.K);
+      fa[x] = block_codes<FULL>(ar, b + x * FEW_WAVES, g, p.K);
+      s[x] = (float)sa[(b + x * FEW_WAVES) * p.sa_ld] * sw[b + x * FEW_WAVES];
     }
 #pragma unroll
-    for (int x = 0; x < U; ++x)
+    for (int x = 0; x < U; ++x) {
+      const f32x4 d = mfma_f8(fw[x], fa[x], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          const f32x4 d = mfma_f8(fw[x][j], fa[x][i], f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[j][i][e] += d[e] * s[x][i];
-        }
+      for (int e = 0; e < 4; ++e) acc[e] += d[e] * s[x];
+    }
   };
   constexpr std::true_type whole_block{};
   constexpr std::integral_constant<int, 1> one{};
   constexpr std::integral_constant<int, 2> two{};
-  constexpr std::integral_constant<int, (MT + NT <= 3 ? 4 : 2)> most{};
+  constexpr std::integral_constant<int, 4> four{};
   const int b0 = z * p.range_blocks, b1 = min(b0 + p.range_blocks, p.KB);
   const int whole = min(b1, p.K / SCALE_BLOCK);
   int b = b0 + wave;
-  for (; b + (most - 1) * WAVES < whole; b += most * WAVES) blocks(whole_block, most, b);
-  if (most > 2 && b + WAVES < whole) {
+  for (; b + 3 * FEW_WAVES < whole; b += 4 * FEW_WAVES) blocks(whole_block, four, b);
+  if (b + FEW_WAVES < whole) {
     blocks(whole_block, two, b);
-    b += 2 * WAVES;
+    b += 2 * FEW_WAVES;
   }
   if (b < whole) blocks(whole_block, one, b);
-  if (whole < b1 && (whole - b0) % WAVES == wave) blocks(std::false_type{}, one, whole);
-#pragma unroll
-  for (int j = 0; j < NT; ++j)
-#pragma unroll
-    for (int i = 0; i < MT; ++i) red[wave][j * MT + i][lane] = acc[j][i];
+  if (whole < b1 && (whole - b0) % FEW_WAVES == wave) blocks(std::false_type{}, one, whole);
+  red[wave][lane] = acc;
   __syncthreads();
-  for (int x = threadIdx.x; x < MT * NT * 64; x += 64 * WAVES) {
-    f32x4 v = red[0][x / 64][x % 64];
+  if (wave > 0 || r >= p.M) return;
+  f32x4 v = red[0][lane];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) v += red[w][x / 64][x % 64];
-    const int j = x / 64 / MT, i = x / 64 % MT, m = 16 * i + x % 16, n = n0 + 16 * j + 4 * (x % 64 / 16);
-    if (!p.part) {
-      store4(p, m, n, v);
-    } else if (m < p.M) {
-      float* q = p.part + ((int64_t)z * p.M + m) * p.N + n;
+  for (int w = 1; w < FEW_WAVES; ++w) v += red[w][lane];
+  const int n = n0 + 4 * g;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (n + e < p.N) q[e] = v[e];
+  for (int e = 0; e < 4; ++e) {
+    if (n + e >= p.N) return;
+    if (p.part) p.part[((int64_t)z * p.M + r) * p.N + n + e] = v[e];
+    else ((__bf16*)p.c)[r * p.c_ld + n + e] = (__bf16)v[e];
+  }
+}
+
+// ---- a wave's piece of the result ---------------------------------------------------------------------
+// 16 MT rows from m0 and 16 NT columns from n0 on: lane l has, of its MT rows m0 + MT (l % 16) + i, the columns 16 j + 4 (l / 16) +
+// 0..3, to be rounded or (PARTS, where there is a buffer for them) added up later.  It passes through LDS (MmResult::BYTES for each wave, free to use) so that rows leave in pieces of 32 NT bytes.
+template <int MT, int NT>
+struct MmResult {
+  static constexpr int ROWS = MT < 4 ? 16 * MT : 64, LD = 32 * NT + 16;       // rows at a time, bytes per row
+  static constexpr int BYTES = ROWS * LD + 64 * MT;
+};
+
+template <int MT, int NT, bool PARTS>
+__device__ __forceinline__ void mm_result(const MmP& p, const f32x4 (&acc)[NT][MT], int z, int m0, int n0, int wave, char* lds) {
+  using T = MmResult<MT, NT>;
+  const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
+  if (PARTS && p.part) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int m = m0 + MT * r + i;
+      if (m >= p.M) continue;
+      float* q = p.part + ((int64_t)z * p.M + m) * p.N;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int n = n0 + 16 * j + 4 * g;
+        if (n + 4 <= p.N) {
+          __builtin_memcpy(q + n, &acc[j][i], 16);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) q[n + e] = acc[j][i][e];
+        }
+      }
+    }
+    return;
+  }
+  char* mine = lds + wave * T::BYTES;
+  constexpr int IR = T::ROWS / 16;     // row tiles that pass through LDS at a time
+  if (16 * NT == SCALE_BLOCK / 2 && p.out_type == SVDMLP_F8) {
+    // largest magnitude of the block of 128 columns of which this wave and its neighbour hold half each
+    float inv[MT];
+    float* largest = (float*)(mine + T::ROWS * T::LD);
+    const float* others = (const float*)(lds + (wave ^ 1) * T::BYTES + T::ROWS * T::LD);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      float x = 0.f;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n0 + 16 * j + 4 * g + e < p.N) x = fmaxf(x, fabsf(acc[j][i][e]));
+      x = fmaxf(x, __shfl_xor(x, 16));
+      x = fmaxf(x, __shfl_xor(x, 32));
+      if (g == 0) largest[16 * i + r] = x;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int m = m0 + MT * r + i;
+      const __bf16 s = scale_of(fmaxf(largest[16 * i + r], others[16 * i + r]));
+      inv[i] = 1.f / (float)s;
+      if (g == 0 && wave % 2 == 0 && m < p.M && n0 < p.N) p.c_scales[(int64_t)(n0 / SCALE_BLOCK) * p.c_scales_ld + m] = s;
+    }
+#pragma unroll
+    for (int i0 = 0; i0 < MT; i0 += IR) {
+#pragma unroll
+      for (int i = i0; i < i0 + IR; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const f32x4 v = acc[j][i];
+          *(unsigned*)(mine + (16 * (i - i0) + r) * T::LD + 16 * j + 4 * g) = codes4(v[0] * inv[i], v[1] * inv[i], v[2] * inv[i], v[3] * inv[i]);
+        }
+      // LDS accesses of a wave are done in order
+#pragma unroll
+      for (int k = 0; k < T::ROWS / (64 / NT); ++k) {
+        const int row = 64 / NT * k + lane / NT, m = m0 + MT * (row % 16) + i0 + row / 16, n = n0 + 16 * (lane % NT);
+        if (m >= p.M || n >= p.N) continue;
+        const u32x4 v = *(const u32x4*)(mine + row * T::LD + 16 * (lane % NT));
+        unsigned char* c = (unsigned char*)p.c + m * p.c_ld + n;
+        if (n + 16 <= p.N) {
+          *(u32x4*)c = v;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (n + e < p.N) c[e] = (unsigned char)(v[e / 4] >> (8 * (e % 4)));
+        }
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int i0 = 0; i0 < MT; i0 += IR) {
+#pragma unroll
+    for (int i = i0; i < i0 + IR; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const f32x4 v = acc[j][i];
+        *(bf16x4*)(mine + (16 * (i - i0) + r) * T::LD + 2 * (16 * j + 4 * g)) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+      }
+    constexpr int L = 2 * NT;            // lanes a row
+#pragma unroll
+    for (int k = 0; k < T::ROWS / (64 / L); ++k) {
+      const int row = 64 / L * k + lane / L, m = m0 + MT * (row % 16) + i0 + row / 16, n = n0 + 8 * (lane % L);
+      if (m >= p.M || n >= p.N) continue;
+      const u32x4 v = *(const u32x4*)(mine + row * T::LD + 16 * (lane % L));
+      __bf16* c = (__bf16*)p.c + m * p.c_ld + n;
+      if (n + 8 <= p.N) {
+        __builtin_memcpy(c, &v, 16);
+      } else {
+        const bf16x8 x = as_bf16x8(v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (n + e < p.N) c[e] = x[e];
+      }
     }
   }
 }
@@ -183,34 +270,31 @@ __device__ __forceinline__ void wait_copies(int t, int steps) {
 // has read those of step t - 1 itself) and its share of the rows of W of step t + 2 (three buffers: the second half read those
 // of step t - 1 in phase 2 t - 1).  Before a step it waits for its A, in the middle of one for its share of the next W,
 // which the first half reads in the next phase.
-template <int MT, int NT, int WM, int WN>
+template <int MT, int NT, int WN>
 struct MmTile {
-  static constexpr int ROWS = 16 * MT * WM, WAVES = WM * WN;     // of the tile, and columns
-  static_assert(WM == 2 && 16 * NT * WN == ROWS && ROWS == 32 * WAVES, "units of equal size, four copies a wave");
+  static constexpr int ROWS = 32 * MT, WAVES = 2 * WN;     // of the tile, and columns
+  static_assert(16 * NT * WN == ROWS && ROWS == 32 * WAVES, "units of equal size, four copies a wave");
   static constexpr int UNIT = ROWS * SCALE_BLOCK;                // rows of A or W of a step
   static constexpr int W_AT = 2 * UNIT;                          // two units for A, then three for W
-  static constexpr int OUT_ROWS = 64, OUT_LD = 32 * NT + 16;     // a wave's piece of the result in LDS, bytes per row
-  static constexpr int OUT = WAVES * OUT_ROWS * OUT_LD, LDS = 5 * UNIT;
-  static_assert(OUT + 4 * WN * ROWS <= LDS, "the result passes through the same memory");
+  static constexpr int LDS = 5 * UNIT;
+  static_assert(WAVES * MmResult<MT, NT>::BYTES <= LDS, "the result passes through the same memory");
 };
 
-template <int MT, int NT, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_mm_tile(MmP p) {
-  using T = MmTile<MT, NT, WM, WN>;
+template <int MT, int NT, int WN>
+__global__ __launch_bounds__(128 * WN) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_mm_tile(MmP p) {
+  using T = MmTile<MT, NT, WN>;
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / WN, wn = wave % WN;
-  const int mtiles = (p.M + T::ROWS - 1) / T::ROWS, ntiles = (p.N + T::ROWS - 1) / T::ROWS, tiles = mtiles * ntiles;
+  const int mtiles = (p.M + T::ROWS - 1) / T::ROWS, ntiles = (p.N + T::ROWS - 1) / T::ROWS;
   int mt, nt;
-  const int id = xcd_contiguous_id(blockIdx.x, gridDim.x), z = __builtin_amdgcn_readfirstlane(id / tiles);
-  banded_tile(id - z * tiles, mtiles, ntiles, p.band, mt, nt);
+  banded_tile(xcd_contiguous_id(blockIdx.x, gridDim.x), mtiles, ntiles, p.band, mt, nt);
   // divisions are done by the vector unit; copies take their addresses from scalar registers
   const int m0 = __builtin_amdgcn_readfirstlane(mt) * T::ROWS, n0 = __builtin_amdgcn_readfirstlane(nt) * T::ROWS;
-  const int b0 = z * p.range_blocks, b1 = min(b0 + p.range_blocks, p.KB);
   const unsigned lds0 = lds_offset_of(lds);
-  // The steps of the range.  A block that ends inside comes first, so that only the prologue has to clear what lies behind it.
-  const int steps = b1 - b0, tail = b1 == p.KB ? p.K % SCALE_BLOCK : 0;
-  auto block_of = [&](int t) { return !tail ? b0 + t : t == 0 ? b1 - 1 : b0 + t - 1; };
+  // A block that ends inside comes first, so that only the prologue has to clear what lies behind it.
+  const int steps = p.KB, tail = p.K % SCALE_BLOCK;
+  auto block_of = [&](int t) { return !tail ? t : t == 0 ? steps - 1 : t - 1; };
 
   // Which row of A is which row of LDS: a lane has row r of each of a wave's MT tiles of 16, and those are MT consecutive rows of
   // the matrix, so that it gets their scales in one load.
@@ -346,112 +430,173 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
   for (int q = Q - LAG; q < Q; ++q) add(q, s_last);
 
-  // ---- result: lane has columns n + 0..3 of row m of every 16 x 16 tile
-  const int mw = m0 + arow, nw = n0 + 16 * NT * wn;
-  if (p.part) {
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int m = mw + MT * r + i;
-      if (m < p.M) {
-        float* q = p.part + ((int64_t)z * p.M + m) * p.N;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const int n = nw + 16 * j + 4 * g;
-          if (n + 4 <= p.N) __builtin_memcpy(q + n, &acc[j][i], 16);
-          else
-            for (int e = 0; e < 4; ++e)
-              if (n + e < p.N) q[n + e] = acc[j][i][e];
-        }
-      }
-    }
-    return;
-  }
   lds_barrier();      // everyone has read the last step
-  const bool f8 = p.out_type == SVDMLP_F8;
-  float* amax_of = (float*)(lds + T::OUT);
-  float inv[MT];
-  if (f8) {
-    // largest magnitude of the block of 128 columns that this wave and its neighbour hold half of each
+  mm_result<MT, NT, false>(p, acc, 0, m0 + arow, n0 + wrow, wave, lds);
+}
+
+// ---- small tiles, three steps in LDS ------------------------------------------------------------------
+// Once 16 bytes a lane, global -> LDS, as above; copy_word: 4 bytes (2: BYTES = 2, into the low half of 4), lane l at lds_dst + 4 l.
+__device__ __forceinline__ void copy1(const char* sbase, unsigned v, unsigned lds_dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0" ::"s"(sbase), "v"(v), "s"(lds_dst) : "memory", "m0");
+}
+template <int BYTES>
+__device__ __forceinline__ void copy_word(const char* sbase, unsigned v, unsigned lds_dst) {
+  if (BYTES == 4)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, %0" ::"s"(sbase), "v"(v), "s"(lds_dst) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %0" ::"s"(sbase), "v"(v), "s"(lds_dst) : "memory", "m0");
+}
+// Four waves, 2 x 2, each with 16 MT rows x 16 NT columns, for results of few tiles, where a CU has one to three workgroups and what
+// counts is a step's chain: wait, barrier, LDS, products.  So a step's operands go from LDS to registers while the step before
+// is multiplied, the copies of two more are on their way (three to seven made no difference), addresses are advanced and not
+// computed, and the scales come by copies as well (4 bytes for each row of A, the weights' scale 64 times), since a wait for a
+// load into a register would wait for the copies issued before it.  Rows x contraction x columns in a graph: 32 x 4096 x 14336
+// 11.4 us (6.6 TB/s of weights without the 2.5 us of a launch), 128 x 2048 x 8192 8.7 us, 256 x 4096 x 4096 13.9 us.
+constexpr int STAGES = 3;
+template <int MT, int NT>
+struct MmRing {
+  static constexpr int TM = 32 * MT, TN = 32 * NT;
+  static constexpr int W_AT = TM * SCALE_BLOCK, SA_AT = W_AT + TN * SCALE_BLOCK, SW_AT = SA_AT + 256, STAGE = SW_AT + 256;
+  static constexpr int CA = TM / 32, CW = TN / 32, COPIES = CA + CW + 1;     // of a wave per step
+  static constexpr int LDS = STAGES * STAGE;
+  static_assert(4 * MmResult<MT, NT>::BYTES <= LDS && TM <= 64 && TN <= SCALE_BLOCK, "one load of scales");
+};
+
+template <int MT, int NT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_mm_ring(MmP p) {
+  using T = MmRing<MT, NT>;
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
+  const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / 2, wn = wave % 2;
+  const int mtiles = (p.M + T::TM - 1) / T::TM, ntiles = (p.N + T::TN - 1) / T::TN, tiles = mtiles * ntiles;
+  // row tiles of the same columns side by side on an XCD, whose L2 then serves the weights to all but the first
+  const int id = xcd_contiguous_id(blockIdx.x, gridDim.x), z = __builtin_amdgcn_readfirstlane(id / tiles);
+  const int nt = __builtin_amdgcn_readfirstlane((id - z * tiles) / mtiles);
+  const int m0 = (id - z * tiles - nt * mtiles) * T::TM, n0 = nt * T::TN;
+  const int b0 = z * p.range_blocks, b1 = min(b0 + p.range_blocks, p.KB);
+  const unsigned lds0 = lds_offset_of(lds);
+  const int steps = b1 - b0, tail = b1 == p.KB ? p.K % SCALE_BLOCK : 0;
+  auto arow_of = [&](int x) { return x / (16 * MT) * (16 * MT) + x % 16 * MT + x % (16 * MT) / 16; };
+  const int cr = lane / 8, cp = (lane % 8) ^ cr;
+  // what the next copies read
+  const int first = tail ? b1 - 1 : b0;
+  const char* anext = p.a + m0 * p.a_ld + (int64_t)first * SCALE_BLOCK;
+  const char* wnext = p.w + n0 * p.w_ld + (int64_t)first * SCALE_BLOCK;
+  const char* snext = wn == 0 ? (const char*)(p.sa + first * p.sa_ld + m0) : (const char*)(p.sw + (int64_t)(n0 / SCALE_BLOCK) * p.KB + first);
+  const int64_t s_step = wn == 0 ? 2 * p.sa_ld : 4;
+  unsigned aoff[T::CA], woff[T::CW];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      float x = 0.f;
+  for (int c = 0; c < T::CA; ++c) aoff[c] = (unsigned)min(arow_of(8 * (wave + 4 * c) + cr), p.M - 1 - m0) * (unsigned)p.a_ld + 16 * cp;
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
+  for (int c = 0; c < T::CW; ++c) woff[c] = (unsigned)min(8 * (wave + 4 * c) + cr, p.N - 1 - n0) * (unsigned)p.w_ld + 16 * cp;
+  const unsigned soff = 2 * min(lane, p.M - 1 - m0);
+  auto issue = [&](int stage, unsigned back) {
+    const unsigned at = lds0 + stage * T::STAGE;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (nw + 16 * j + 4 * g + e < p.N) x = fmaxf(x, fabsf(acc[j][i][e]));
-      x = fmaxf(x, __shfl_xor(x, 16));
-      x = fmaxf(x, __shfl_xor(x, 32));
-      if (g == 0) amax_of[wn * T::ROWS + arow + 16 * i + r] = x;
-    }
-    __syncthreads();
+    for (int c = 0; c < T::CA; ++c) copy1(anext, aoff[c] - back, at + 1024 * (wave + 4 * c));
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int row = arow + 16 * i + r, m = mw + MT * r + i;
-      const __bf16 s = scale_of(fmaxf(amax_of[wn * T::ROWS + row], amax_of[(wn ^ 1) * T::ROWS + row]));
-      inv[i] = 1.f / (float)s;
-      if (g == 0 && wn % 2 == 0 && m < p.M && nw < p.N) p.c_scales[(int64_t)(nw / SCALE_BLOCK) * p.c_scales_ld + m] = s;
+    for (int c = 0; c < T::CW; ++c) copy1(wnext, woff[c] - back, at + T::W_AT + 1024 * (wave + 4 * c));
+    if (wn == 0) copy_word<2>(snext, soff, at + T::SA_AT);
+    else copy_word<4>(snext, 0, at + T::SW_AT);
+    anext += SCALE_BLOCK;
+    wnext += SCALE_BLOCK;
+    snext += s_step;
+  };
+  issue(0, tail ? (unsigned)max(0, 16 * cp - ((tail - 1) & ~15)) : 0u);
+  if (tail) {
+    anext += (b0 - b1) * SCALE_BLOCK;      // back to the first block
+    wnext += (b0 - b1) * SCALE_BLOCK;
+    snext += (b0 - b1) * s_step;
+    wait_vmcnt<0>();
+    for (int c = 0; c < T::CA + T::CW; ++c) {       // clear what this lane brought beyond the end of the contraction
+      u32x4* q = (u32x4*)(lds + 1024 * (wave + 4 * c) + lane * 16);
+      u32x4 v = *q;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int l = tail - 16 * cp - 4 * i;
+        v[i] = l >= 4 ? v[i] : l <= 0 ? 0u : v[i] & (0xffffffffu >> (32 - 8 * l));
+      }
+      *q = v;
     }
   }
-  char* mine = lds + wave * T::OUT_ROWS * T::OUT_LD;
-  static_assert(16 * NT == 64, "two waves hold a block of 128 columns; 128 bytes of bf16 in a row's piece");
-  constexpr int IR = T::OUT_ROWS / 16;     // row tiles that pass through LDS at a time
 #pragma unroll
-  for (int i0 = 0; i0 < MT; i0 += IR) {
+  for (int t = 1; t < STAGES; ++t)
+    if (t < steps) issue(t, 0);
+
+  const int at0 = r * SCALE_BLOCK + 16 * (g ^ (r % 8)), at1 = r * SCALE_BLOCK + 16 * ((4 + g) ^ (r % 8));
+  const int arow = 16 * MT * wm, wrow = 16 * NT * wn;
+  auto frag = [&](int at) { return join16(*(const u32x4*)(lds + at + at0), *(const u32x4*)(lds + at + at1)); };
+  // A step's operands are read from LDS while the step before is multiplied; its place in LDS is then free.
+  struct Step {
+    i32x8 w[NT], a[MT];
+    unsigned sa[MT];
+    float sw;
+  };
+  auto read = [&](Step& x, int stage) {
+    const int at = stage * T::STAGE;
 #pragma unroll
-    for (int i = i0; i < i0 + IR; ++i)
+    for (int i = 0; i < MT; ++i) x.a[i] = frag(at + (arow + 16 * i) * SCALE_BLOCK);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        char* q = mine + (16 * (i - i0) + r) * T::OUT_LD;
-        const f32x4 v = acc[j][i];
-        if (f8) *(unsigned*)(q + 16 * j + 4 * g) = codes4(v[0] * inv[i], v[1] * inv[i], v[2] * inv[i], v[3] * inv[i]);
-        else *(bf16x4*)(q + 2 * (16 * j + 4 * g)) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+    for (int j = 0; j < NT; ++j) x.w[j] = frag(at + T::W_AT + (wrow + 16 * j) * SCALE_BLOCK);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) x.sa[i] = *(const unsigned*)(lds + at + T::SA_AT + 4 * (arow + MT * r + i));
+    x.sw = *(const float*)(lds + at + T::SW_AT + 4 * lane);
+  };
+  f32x4 acc[NT][MT] = {};
+  int stage = 0;                      // of step t
+  auto step = [&](int t, const Step& now, Step& next) {
+    wait_copies<T::COPIES>(t + 2, steps);      // those of step t + 1 have landed
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    lds_barrier();
+    if (t + STAGES < steps) issue(stage, 0);
+    stage = stage + 1 < STAGES ? stage + 1 : 0;
+    read(next, stage);                // past the last step: not used
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 d[NT][MT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) d[j][i] = mfma_f8(now.w[j], now.a[i], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const float s = __builtin_bit_cast(float, now.sa[i] << 16) * now.sw;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][i][e] += d[j][i][e] * s;
       }
-    // LDS of the same wave: in order
-    if (f8) {
-#pragma unroll
-      for (int k = 0; k < T::OUT_ROWS / 16; ++k) {
-        const int row = 16 * k + lane / 4, m = mw + MT * (row % 16) + i0 + row / 16, n = nw + 16 * (lane % 4);
-        if (m >= p.M || n >= p.N) continue;
-        const u32x4 v = *(const u32x4*)(mine + row * T::OUT_LD + 16 * (lane % 4));
-        unsigned char* c = (unsigned char*)p.c + m * p.c_ld + n;
-        if (n + 16 <= p.N) *(u32x4*)c = v;
-        else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (n + e < p.N) c[e] = (unsigned char)(v[e / 4] >> (8 * (e % 4)));
-        }
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < T::OUT_ROWS / 8; ++k) {
-        const int row = 8 * k + lane / 8, m = mw + MT * (row % 16) + i0 + row / 16, n = nw + 8 * (lane % 8);
-        if (m >= p.M || n >= p.N) continue;
-        const u32x4 v = *(const u32x4*)(mine + row * T::OUT_LD + 16 * (lane % 8));
-        __bf16* c = (__bf16*)p.c + m * p.c_ld + n;
-        if (n + 8 <= p.N) __builtin_memcpy(c, &v, 16);
-        else {
-          const bf16x8 x = as_bf16x8(v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (n + e < p.N) c[e] = x[e];
-        }
-      }
-    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  Step even, odd;
+  wait_copies<2 * T::COPIES>(2, steps);
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  lds_barrier();
+  read(even, 0);
+  for (int t = 0; t < steps; t += 2) {
+    step(t, even, odd);
+    if (t + 1 < steps) step(t + 1, odd, even);
   }
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  lds_barrier();      // everyone has read the last step
+  mm_result<MT, NT, true>(p, acc, z, m0 + arow, n0 + wrow, wave, lds);
 }
 
 // Adds the ranges' partial sums in their order and rounds: 16 lanes hold 128 columns of a row, a workgroup 16 rows of them.
+template <int JOIN>      // ranges whose loads are issued together
 __global__ __launch_bounds__(256) void k_mm_join(MmP p) {
   const int lane = threadIdx.x % 16, nb = (p.N + SCALE_BLOCK - 1) / SCALE_BLOCK;
   const int m = (int)(blockIdx.x / nb) * 16 + threadIdx.x / 16, b = (int)(blockIdx.x % nb), n = b * SCALE_BLOCK + 8 * lane;
   if (m >= p.M) return;
   float v[8] = {};
   if (n < p.N)
-    for (int z = 0; z < p.ranges; ++z) {
-      const Raw8<float> x = load8(p.part + ((int64_t)z * p.M + m) * p.N, n, p.N);
+    for (int z = 0; z < p.ranges; z += JOIN) {
+      Raw8<float> x[JOIN];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += x.get(e);
+      for (int i = 0; i < JOIN; ++i) x[i] = z + i < p.ranges ? load8(p.part + ((int64_t)(z + i) * p.M + m) * p.N, n, p.N) : Raw8<float>{};
+#pragma unroll
+      for (int i = 0; i < JOIN; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += x[i].get(e);
     }
   if (p.out_type == SVDMLP_F8) {
     float amax = 0.f;
@@ -466,79 +611,95 @@ __global__ __launch_bounds__(256) void k_mm_join(MmP p) {
 }
 
 // ---- host -------------------------------------------------------------------------------------------
-enum { MM_FEW = 0, MM_TILE_128 = 1, MM_TILE_256 = 2 };
+// Which kernel, and into how many ranges the contraction is cut: the least time by a model of the compute units.  A
+// workgroup's steps take `step` us where it has a CU to itself (its own chain of waits), `share` us each where `per_cu` of them
+// share one (the CU's copies and matrix products), a tile besides `tile` us for its first copies and its result, a launch
+// LAUNCH_US; cut contractions and 8-bit results of 64-column tiles add a second launch that reads the partial sums.  The figures
+// are fitted to launches in a graph; model / measured us of the kernel chosen and the next best, rows x contraction x columns:
+//   16 x 4096 x 14336     ring 32x64 11.2 / 11.3, few 14.6 / 13.5        128 x 2048 x 8192  ring 32x64 8.7 / 8.7, ring 64x64 8.6 / 8.9
+//   256 x 4096 x 4096     ring 64x64 14.0 / 13.9, ring 64x128 18.0 / 18.3  1024 x 4096 x 4096  ring 64x128 26.9 / 25.6, tile 128 29.5 / 27.8
+//   512 x 4096 x 14336    tile 128 43 / 38, ring 64x128 51 / 45          4096 x 8192 x 16384 tile 256 462 / 437, tile 128 630 / 590
+enum { MM_FEW = 0, MM_RING_32, MM_RING_64, MM_RING_64_128, MM_TILE_128, MM_TILE_256, MM_KINDS };
+struct MmKind {
+  const char* name;
+  int rows, cols, max_rows;      // of a tile; rows of A that it takes (0: any)
+  double step, share, tile;
+};
+constexpr MmKind MM_KIND[MM_KINDS] = {
+    {"k_mm_few[tile=16x16", 16, 16, 16, 0.62 / FEW_WAVES, 0.60 / FEW_WAVES, 0.},
+    {"k_mm_ring[tile=32x64", 32, 64, 0, 0.26, 0.17, 0.4},
+    {"k_mm_ring[tile=64x64", 64, 64, 0, 0.34, 0.235, 0.6},
+    {"k_mm_ring[tile=64x128", 64, 128, 0, 0.45, 0.35, 1.0},
+    {"k_mm_tile[tile=128x128", 128, 128, 0, 0.775, 0.57, 2.2},
+    {"k_mm_tile[tile=256x256", 256, 256, 0, 1.7, 1.7, 6.0},
+};
+constexpr double LAUNCH_US = 2.5, JOIN_US = 2.3, HBM_BYTES_PER_US = 6.8e6, PART_BYTES_PER_US = 4.0e6;
+constexpr int MM_CUS = 256;      // the model's device, so that a result's order of sums goes by the extents alone
+
 struct MmPlan {
-  int kernel;
-  int mt, nt, waves;          // MM_FEW
-  int ranges, range_blocks;
+  int kind, ranges, range_blocks;
   bool join;                  // partial sums that k_mm_join adds and rounds
   int64_t tiles;
+  double est_us;
 };
 
-
-static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, MmPlan* q) {
+static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, MmPlan* best) {
   if (M < 0 || N <= 0 || K <= 0) return SVDMLP_INVALID_ARGUMENT;
   if (out_type != SVDMLP_F8 && out_type != SVDMLP_BF16) return SVDMLP_INVALID_ARGUMENT;
   if (M >= int64_t(1) << 24 || N > int64_t(1) << 22 || K > int64_t(1) << 22) return SVDMLP_UNSUPPORTED;
   const int KB = (int)scale_blocks(K);
-  *q = MmPlan{};
-  int ranges = 1;
-  int few_max = 64;
-  if (M <= few_max) {
-    q->kernel = MM_FEW;
-    q->mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    q->nt = 4;
-    while (q->nt > 1 && (N + 16 * q->nt - 1) / (16 * q->nt) < 256) q->nt /= 2;
-    q->tiles = (N + 16 * q->nt - 1) / (16 * q->nt);
-    q->waves = q->tiles <= 256 && KB >= 32 && q->mt * q->nt <= 8 ? 16 : 8;
-    if (out_type == SVDMLP_F8) {
-      while (q->tiles * ranges < 256 && ranges * 2 * q->waves <= KB) ranges *= 2;
-      q->join = true;
+  best->kind = -1;
+  for (int k = 0; k < MM_KINDS; ++k) {
+    const MmKind& kind = MM_KIND[k];
+    if (kind.max_rows && M > kind.max_rows) continue;
+    const int64_t tiles = ((M + kind.rows - 1) / kind.rows) * ((N + kind.cols - 1) / kind.cols);
+    for (int r = 1; r <= (k < MM_TILE_128 ? 32 : 1) && r <= KB; r *= 2) {     // the tile kernels take whole contractions
+      MmPlan q;
+      q.kind = k;
+      q.tiles = tiles;
+      q.range_blocks = (KB + r - 1) / r;
+      q.ranges = (KB + q.range_blocks - 1) / q.range_blocks;
+      if (q.ranges != r && r > 1) continue;
+      if (tiles * r >= int64_t(1) << 22) continue;        // a grid of 512 lanes each, below 2^31
+      q.join = r > 1 || (out_type == SVDMLP_F8 && kind.cols < SCALE_BLOCK);
+      const double per_cu = (double)((tiles * r + MM_CUS - 1) / MM_CUS);
+      double step = kind.step, share = kind.share;
+      int steps = q.range_blocks;
+      if (k == MM_FEW) {       // eight waves take a block each; every workgroup reads the rows of A
+        steps = (steps + FEW_WAVES - 1) / FEW_WAVES * FEW_WAVES;
+        step += 0.022 / FEW_WAVES * M;
+        share += 0.022 / FEW_WAVES * M;
+      }
+      double t = kind.tile * per_cu + steps * (step > share * per_cu ? step : share * per_cu);
+      const double bytes = (double)N * K + (double)M * K + (double)M * N * (out_type == SVDMLP_F8 ? 1 : 2);
+      if (t < bytes / HBM_BYTES_PER_US) t = bytes / HBM_BYTES_PER_US;
+      q.est_us = LAUNCH_US + t + (q.join ? JOIN_US + 8. * M * N * r / PART_BYTES_PER_US : 0.);
+      if (best->kind < 0 || q.est_us < best->est_us) *best = q;
     }
-  } else {
-    const int64_t t256 = (M + 255) / 256 * ((N + 255) / 256), t128 = (M + 127) / 128 * ((N + 127) / 128);
-    q->kernel = t256 >= 200 ? MM_TILE_256 : MM_TILE_128;
-    q->tiles = q->kernel == MM_TILE_256 ? t256 : t128;
-    const int slots = q->kernel == MM_TILE_256 ? 256 : 512;
-    while (q->tiles * ranges * 2 <= slots && KB / (ranges * 2) >= 4) ranges *= 2;
   }
-  q->range_blocks = (KB + ranges - 1) / ranges;
-  q->ranges = (KB + q->range_blocks - 1) / q->range_blocks;
-  if (q->ranges > 1) q->join = true;
-  if (q->tiles * q->ranges >= int64_t(1) << 22) return SVDMLP_UNSUPPORTED;    // a grid of 1024 lanes each, below 2^32
-  return SVDMLP_OK;
+  return best->kind < 0 ? SVDMLP_UNSUPPORTED : SVDMLP_OK;
 }
 
 static size_t part_bytes(const MmPlan& q, int64_t M, int64_t N) { return q.join ? (size_t)q.ranges * M * N * 4 : 0; }
 
-template <int MT, int NT>
-static void run_few(const MmP& p, const MmPlan& q, hipStream_t st) {
-  const unsigned wgs = (unsigned)(q.tiles * q.ranges);
-  if (q.waves == 16) {
-    if constexpr (MT * NT <= 8) k_mm_few<MT, NT, 16><<<wgs, 1024, 0, st>>>(p);
-  }
-  else if (q.waves == 8) k_mm_few<MT, NT, 8><<<wgs, 512, 0, st>>>(p);
-  else k_mm_few<MT, NT, 4><<<wgs, 256, 0, st>>>(p);
-}
-template <int MT>
-static void run_few(const MmP& p, const MmPlan& q, hipStream_t st) {
-  if (q.nt == 1) run_few<MT, 1>(p, q, st);
-  else if (q.nt == 2) run_few<MT, 2>(p, q, st);
-  else run_few<MT, 4>(p, q, st);
+static void launch_join(const MmP& p, hipStream_t st) {
+  const unsigned wgs = (unsigned)((p.M + 15) / 16 * scale_blocks(p.N));
+  if (p.ranges == 1) k_mm_join<1><<<wgs, 256, 0, st>>>(p);
+  else if (p.ranges <= 4) k_mm_join<4><<<wgs, 256, 0, st>>>(p);
+  else k_mm_join<8><<<wgs, 256, 0, st>>>(p);
 }
 
 static void launch_mm(MmP& p, const MmPlan& q, hipStream_t st) {
-  if (q.kernel == MM_FEW) {
-    if (q.mt == 1) run_few<1>(p, q, st);
-    else if (q.mt == 2) run_few<2>(p, q, st);
-    else run_few<4>(p, q, st);
-    return;
-  }
   const unsigned wgs = (unsigned)(q.tiles * q.ranges);
-  const int rows = q.kernel == MM_TILE_256 ? 256 : 128;
-  p.band = band_height((p.M + rows - 1) / rows, wgs);
-  if (q.kernel == MM_TILE_256) k_mm_tile<8, 4, 2, 4><<<wgs, 512, 0, st>>>(p);
-  else k_mm_tile<4, 4, 2, 2><<<wgs, 256, 0, st>>>(p);
+  p.band = band_height((p.M + MM_KIND[q.kind].rows - 1) / MM_KIND[q.kind].rows, wgs);
+  switch (q.kind) {
+    case MM_FEW: k_mm_few<<<wgs, 64 * FEW_WAVES, 0, st>>>(p); break;
+    case MM_RING_32: k_mm_ring<1, 2><<<wgs, 256, 0, st>>>(p); break;
+    case MM_RING_64: k_mm_ring<2, 2><<<wgs, 256, 0, st>>>(p); break;
+    case MM_RING_64_128: k_mm_ring<2, 4><<<wgs, 256, 0, st>>>(p); break;
+    case MM_TILE_128: k_mm_tile<4, 4, 2><<<wgs, 256, 0, st>>>(p); break;
+    default: k_mm_tile<8, 4, 4><<<wgs, 512, 0, st>>>(p); break;
+  }
 }
 
 }  // namespace svdmlp
@@ -557,13 +718,8 @@ int svdmlp_scaled_matmul_describe(int64_t M, int64_t N, int64_t K, int32_t out_t
   buf[0] = 0;
   MmPlan q;
   if (const int st = plan_mm(M, N, K, out_type, &q)) return st;
-  int n;
-  if (q.kernel == MM_FEW)
-    n = std::snprintf(buf, buf_bytes, "k_mm_few[tile=%dx%d tiles=%lld waves=%d ranges=%d]%s", 16 * q.mt, 16 * q.nt, (long long)q.tiles,
-                      q.waves, q.ranges, q.join ? " k_mm_join" : "");
-  else
-    n = std::snprintf(buf, buf_bytes, "k_mm_tile[tile=%s tiles=%lld ranges=%d]%s", q.kernel == MM_TILE_256 ? "256x256" : "128x128",
-                      (long long)q.tiles, q.ranges, q.join ? " k_mm_join" : "");
+  const int n = std::snprintf(buf, buf_bytes, "%s tiles=%lld ranges=%d est_us=%.1f]%s", MM_KIND[q.kind].name, (long long)q.tiles, q.ranges,
+                              q.est_us, q.join ? " k_mm_join" : "");
   return n > 0 && (size_t)n < buf_bytes ? SVDMLP_OK : SVDMLP_INVALID_ARGUMENT;
 }
 
@@ -596,7 +752,7 @@ int svdmlp_scaled_matmul(const svdmlp_scaled_matmul_args* a, void* hip_stream) {
   p.ranges = q.ranges; p.range_blocks = q.range_blocks;
   hipStream_t st = (hipStream_t)hip_stream;
   launch_mm(p, q, st);
-  if (q.join) k_mm_join<<<(unsigned)((p.M + 15) / 16 * scale_blocks(p.N)), 256, 0, st>>>(p);
+  if (q.join) launch_join(p, st);
   return launch_status();
 }
 
