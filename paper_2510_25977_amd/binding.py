@@ -7,6 +7,7 @@ or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import struct
 from pathlib import Path
 from typing import NamedTuple, Optional
@@ -373,51 +374,66 @@ def empty_scaled(rows: int, cols: int, device, block_rows: int = 1) -> Scaled:
     return Scaled(codes, torch.empty((-(-rows // SCALE_BLOCK), blocks), dtype=torch.float32, device=device))
 
 
-_F8 = torch.float8_e4m3fn
+_F8, _BF16 = torch.float8_e4m3fn, torch.bfloat16
 
 
-def _rows(t: torch.Tensor, what: str, shape, dtype, device, multiple: int = 1):
+# The smallest calls are bound by what follows, so it asks a tensor for little: 0.4 us each.
+def _refuse(t, what: str, shape, dtype, device: int):
+    raise ValueError(f"{what} must be a {tuple(shape)} {dtype} tensor on cuda:{device} whose rows lie in one piece, "
+                     f"got {tuple(t.shape)} {t.dtype} on {t.device} with strides {t.stride()}")
+
+
+def _rows(t: torch.Tensor, what: str, shape, dtype, device: int, multiple: int = 1):
     """(address, row stride) of a matrix on `device`: rows of consecutive elements, any stride between them."""
-    if not (t.dim() == 2 and t.shape == shape and t.dtype == dtype and t.device == device and (t.stride(1) == 1 or shape[1] == 1)):
-        raise ValueError(f"{what} must be a {tuple(shape)} {dtype} matrix on {device} whose rows lie in one piece, "
-                         f"got {tuple(t.shape)} {t.dtype} on {t.device} with strides {t.stride()}")
+    stride = t.stride()
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or (stride[1] != 1 and shape[1] != 1):
+        _refuse(t, what, shape, dtype, device)
     # the stride of a single row says nothing
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else (shape[1] + multiple - 1) // multiple * multiple
+    return t.data_ptr(), stride[0] if shape[0] > 1 else (shape[1] + multiple - 1) // multiple * multiple
 
 
-def _vector(t: Optional[torch.Tensor], what: str, n: int, dtype, device) -> int:
+def _vector(t: Optional[torch.Tensor], what: str, n: int, dtype, device: int) -> int:
     if t is None:
         return 0
-    if not (t.dim() == 1 and t.shape[0] == n and t.dtype == dtype and t.device == device and (t.stride(0) == 1 or n == 1)):
-        raise ValueError(f"{what} must be a contiguous {dtype} vector of {n} on {device}")
+    if t.shape != (n,) or t.dtype is not dtype or t.get_device() != device or (n > 1 and t.stride()[0] != 1):
+        _refuse(t, what, (n,), dtype, device)
     return t.data_ptr()
 
 
-def _codes(t, what: str, shape, device, weights: bool = False):
-    """(codes, codes stride, scales, scales stride)"""
+def _codes(t, what: str, shape, device: int):
+    """(codes, codes stride, scales, scales stride) of activations"""
     codes, scales = t
     ptr, ld = _rows(codes, what, shape, _F8, device, 16)
-    blocks = -(-shape[1] // SCALE_BLOCK)
-    if weights:
-        want = (-(-shape[0] // SCALE_BLOCK), blocks)
-        if not (scales.shape == want and scales.is_contiguous() and scales.dtype == torch.float32 and scales.device == device):
-            raise ValueError(f"the scales of {what} must be a contiguous float32 {want} on {device}")
-        return ptr, ld, scales.data_ptr(), blocks
-    sptr, sld = _rows(scales, f"the scales of {what}", (blocks, shape[0]), torch.bfloat16, device)
-    return ptr, ld, sptr, max(sld, shape[0])
+    rows = shape[0]
+    sptr, sld = _rows(scales, "the scales of " + what, ((shape[1] + SCALE_BLOCK - 1) // SCALE_BLOCK, rows), _BF16, device)
+    return ptr, ld, sptr, sld if sld > rows else rows
 
 
-def _device_of(t: torch.Tensor, what: str):
-    if not (t.is_cuda and t.dim() == 2):
+def _weight_codes(t, what: str, shape, device: int):
+    """(codes, codes stride, scales) of weights"""
+    codes, scales = t
+    ptr, ld = _rows(codes, what, shape, _F8, device, 16)
+    want = (-(-shape[0] // SCALE_BLOCK), -(-shape[1] // SCALE_BLOCK))
+    sptr, sld = _rows(scales, "the scales of " + what, want, torch.float32, device)
+    if sld != want[1]:
+        _refuse(scales, "the (contiguous) scales of " + what, want, torch.float32, device)
+    return ptr, ld, sptr
+
+
+def _device_of(t: torch.Tensor, what: str) -> int:
+    if not t.is_cuda or t.dim() != 2:
         raise ValueError(f"{what} must be a matrix on the GPU")
-    return t.device
+    return t.get_device()
 
 
-def _run(name: str, rows: int, args: bytes, device, stream) -> None:
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _run(name: str, rows: int, args: bytes, device: int, stream) -> None:
     if rows == 0:            # a tensor of no rows has no address
         return
-    s = _current_raw_stream(device.index) if stream is None else stream.cuda_stream
-    if device.index != torch.cuda.current_device():   # kernels are launched on the current device
+    s = _current_raw_stream(device) if stream is None else stream.cuda_stream
+    if device != _current_device():          # kernels are launched on the current device
         with torch.cuda.device(device):
             st = getattr(lib(), name)(args, s)
     else:
@@ -430,31 +446,33 @@ def quantize(x: torch.Tensor, gate_with: Optional[torch.Tensor] = None, *, block
              stream: Optional[torch.cuda.Stream] = None) -> Scaled:
     """x, or SiLU(x) * gate_with, as e4m3 codes with a scale per row and 128 columns (``block_rows=128``: weights, one per
     128 x 128).  x: [R, C] bfloat16 or float32."""
-    dev = _device_of(x, "x")
-    if x.dtype not in _TORCH_DTYPE:
+    dev, shape, dtype = _device_of(x, "x"), x.shape, x.dtype
+    if dtype not in _TORCH_DTYPE:
         raise ValueError("x must be bfloat16 or float32")
-    R, C = x.shape
-    xp, xld = _rows(x, "x", x.shape, x.dtype, dev)
-    gp, gld = (0, 0) if gate_with is None else _rows(gate_with, "gate_with", x.shape, x.dtype, dev)
+    R, C = shape
+    xp, xld = _rows(x, "x", shape, dtype, dev)
+    gp, gld = (0, 0) if gate_with is None else _rows(gate_with, "gate_with", shape, dtype, dev)
     if out is None:
-        out = empty_scaled(R, C, dev, block_rows)
-    cp, cld, sp, sld = _codes(out, "out", x.shape, dev, block_rows != 1)
-    _run("svdmlp_quantize", R, QUANTIZE_ARGS.pack(R, C, _TORCH_DTYPE[x.dtype], block_rows, xp, gp, xld, gld, cp, sp, cld, sld), dev, stream)
+        out = empty_scaled(R, C, x.device, block_rows)
+    if block_rows == 1:
+        cp, cld, sp, sld = _codes(out, "out", shape, dev)
+    else:
+        (cp, cld, sp), sld = _weight_codes(out, "out", shape, dev), 0
+    _run("svdmlp_quantize", R, QUANTIZE_ARGS.pack(R, C, _TORCH_DTYPE[dtype], block_rows, xp, gp, xld, gld, cp, sp, cld, sld), dev, stream)
     return Scaled(*out)
 
 
 def _norm(branch, residual, weight, bias, kind, eps, weight_plus, residual_scale, branch_scale, gate, gate_rows, gate_act,
           next_weight, next_bias, next_kind, next_eps, h, out, scaled, want_h, stream):
-    stream_t = residual if residual is not None else branch
-    dev = _device_of(stream_t, "x")
-    shape = stream_t.shape
+    x = residual if residual is not None else branch      # of the residual stream's type
+    dev, shape, stream_dtype = _device_of(x, "x"), x.shape, x.dtype
     M, d = shape
     # the type of everything but the residual stream
-    of = next((t for t in (branch, weight, next_weight, bias, next_bias) if t is not None), None)
-    dtype = of.dtype if of is not None else stream_t.dtype
-    if dtype not in _TORCH_DTYPE or stream_t.dtype not in _TORCH_DTYPE:
+    of = branch if branch is not None else weight if weight is not None else next_weight
+    dtype = of.dtype if of is not None else bias.dtype if bias is not None else next_bias.dtype if next_bias is not None else stream_dtype
+    if dtype not in _TORCH_DTYPE or stream_dtype not in _TORCH_DTYPE:
         raise ValueError("inputs must be bfloat16 or float32")
-    rp, rld = (0, 0) if residual is None else _rows(residual, "residual", shape, residual.dtype, dev)
+    rp, rld = (0, 0) if residual is None else _rows(residual, "residual", shape, stream_dtype, dev)
     bp, bld = (0, 0) if branch is None else _rows(branch, "branch", shape, dtype, dev)
     gp = gld = 0
     if gate is not None:
@@ -462,13 +480,13 @@ def _norm(branch, residual, weight, bias, kind, eps, weight_plus, residual_scale
             raise ValueError("gate_rows must be at least 1")
         gp, gld = _rows(gate, "gate", (-(-M // gate_rows), d), dtype, dev)
     if h is None and want_h:
-        h = torch.empty((M, d), dtype=stream_t.dtype, device=dev)
-    hp, hld = (0, 0) if h is None else _rows(h, "h", shape, stream_t.dtype, dev)
+        h = torch.empty((M, d), dtype=stream_dtype, device=x.device)
+    hp, hld = (0, 0) if h is None else _rows(h, "h", shape, stream_dtype, dev)
     op = old = sp = sld = 0
     out_type = _TORCH_DTYPE[dtype]
     if next_kind != NORM_NONE:
         if out is None:
-            out = empty_scaled(M, d, dev) if scaled else torch.empty((M, d), dtype=dtype, device=dev)
+            out = empty_scaled(M, d, x.device) if scaled else torch.empty((M, d), dtype=dtype, device=x.device)
         if isinstance(out, tuple):
             out_type = SVDMLP_F8
             op, old, sp, sld = _codes(out, "out", shape, dev)
@@ -476,7 +494,7 @@ def _norm(branch, residual, weight, bias, kind, eps, weight_plus, residual_scale
         else:
             op, old = _rows(out, "out", shape, dtype, dev)
     args = NORM_ARGS.pack(
-        M, d, _TORCH_DTYPE[dtype], _TORCH_DTYPE[stream_t.dtype], out_type, kind, next_kind, gate_act, gate_rows, eps, next_eps,
+        M, d, _TORCH_DTYPE[dtype], _TORCH_DTYPE[stream_dtype], out_type, kind, next_kind, gate_act, gate_rows, eps, next_eps,
         weight_plus, residual_scale, rp, bp, rld, bld, _vector(weight, "weight", d, dtype, dev), _vector(bias, "bias", d, dtype, dev),
         _vector(branch_scale, "branch_scale", d, dtype, dev), gp, gld, _vector(next_weight, "next_weight", d, dtype, dev),
         _vector(next_bias, "next_bias", d, dtype, dev), hp, hld, op, old, sp, sld)
@@ -511,6 +529,7 @@ def norm_out(branch: torch.Tensor, residual: Optional[torch.Tensor] = None, weig
                  next_weight, next_bias, next_kind, eps if next_eps is None else next_eps, h, out, scaled, True, stream)
 
 
+@functools.lru_cache(maxsize=4096)
 def svdmlp_scaled_matmul_workspace_bytes(M: int, N: int, K: int, out_type: int) -> int:
     return int(lib().svdmlp_scaled_matmul_workspace_bytes(int(M), int(N), int(K), int(out_type)))
 
@@ -525,35 +544,35 @@ def scaled_matmul(a, w, *, out=None, out_dtype: torch.dtype = torch.bfloat16, st
     """a [M, K] times the transpose of w [N, K], both ``Scaled`` (or pairs of codes and scales): activations with a scale per
     row and 128 columns, weights with one per 128 x 128.  The result [M, N] is ``out`` or a new tensor of ``out_dtype``;
     torch.float8_e4m3fn (or a ``Scaled`` as ``out``) makes it the next product's activations."""
-    dev = _device_of(a[0], "a")
-    M, K = a[0].shape
-    if w[0].dim() != 2 or w[0].shape[1] != K:
+    codes = a[0]
+    dev, shape = _device_of(codes, "a"), codes.shape
+    M, K = shape
+    if w[0].dim() != 2:
         raise ValueError(f"w must be [N, {K}]")
     N = w[0].shape[0]
-    ap, ald, asp, asld = _codes(a, "a", (M, K), dev)
-    wp, wld, wsp, _ = _codes(w, "w", (N, K), dev, True)
+    ap, ald, asp, asld = _codes(a, "a", shape, dev)
+    wp, wld, wsp = _weight_codes(w, "w", (N, K), dev)
     if out is None:
-        if out_dtype not in (torch.bfloat16, _F8):
+        if out_dtype is not _BF16 and out_dtype is not _F8:
             raise ValueError("out_dtype must be bfloat16 or float8_e4m3fn")
-        out = empty_scaled(M, N, dev) if out_dtype == _F8 else torch.empty((M, N), dtype=out_dtype, device=dev)
-    csp = csld = 0
+        out = empty_scaled(M, N, codes.device) if out_dtype is _F8 else torch.empty((M, N), dtype=_BF16, device=codes.device)
+    out_type, csp, csld = SVDMLP_BF16, 0, 0
     if isinstance(out, tuple):
         out_type = SVDMLP_F8
         cp, cld, csp, csld = _codes(out, "out", (M, N), dev)
         out = Scaled(*out)
     else:
-        out_type = SVDMLP_BF16
-        cp, cld = _rows(out, "out", (M, N), torch.bfloat16, dev)
-    need = lib().svdmlp_scaled_matmul_workspace_bytes(M, N, K, out_type)
-    ws = None
+        cp, cld = _rows(out, "out", (M, N), _BF16, dev)
+    need, ws = svdmlp_scaled_matmul_workspace_bytes(M, N, K, out_type), 0
     if need:
         if stream is None:
-            ws = torch.empty(need, dtype=torch.uint8, device=dev)
+            space = torch.empty(need, dtype=torch.uint8, device=codes.device)
         else:                        # of the stream that uses it, so that it is not handed out again too early
             with torch.cuda.stream(stream):
-                ws = torch.empty(need, dtype=torch.uint8, device=dev)
+                space = torch.empty(need, dtype=torch.uint8, device=codes.device)
+        ws = space.data_ptr()
     _run("svdmlp_scaled_matmul", M, SCALED_MATMUL_ARGS.pack(M, N, K, out_type, 0, ap, asp, ald, asld, wp, wsp, wld, cp, csp, cld, csld,
-                                                         ws.data_ptr() if need else 0, need), dev, stream)
+                                                            ws, need), dev, stream)
     return out
 
 

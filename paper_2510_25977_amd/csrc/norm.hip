@@ -1,7 +1,8 @@
 // The norms around a block of the residual stream, with the residual, the gate and the scales, in one pass:
 //   b = [norm(branch) (weight + plus) + bias] branch_scale act(gate)    h = residual_scale residual + b    out = norm(h) ..
 // A row lies in the registers of its threads in fp32 from its first load to its last store, so every input is read once and
-// every result written once; two or three bytes move per instruction and element, so HBM bounds it.
+// every result written once, and HBM bounds it: 4096 x 4096 with a residual into 8 bits 117 MB in 26.3 us (4.5 TB/s; a copy of
+// 2 GiB moves 4.8), 8192 x 5120 with an fp32 residual 503 MB in 91 us (5.5 TB/s), with a tanh gate and scale 109 us.
 #include "scaled.h"
 
 namespace svdmlp {
@@ -58,35 +59,37 @@ __device__ __forceinline__ void normalize(float (&v)[NV][8], int kind, float eps
     for (int e = 0; e < 8; ++e) v[i][e] *= scale;
 }
 
-template <class T>
-__device__ __forceinline__ void affine(float (&x)[8], const void* weight, const void* bias, int col, const NormP& p) {
-  if (weight) {
-    const Raw8<T> w = load8((const T*)weight, col, p.d);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= w.get(e) + p.weight_plus;
-  }
-  if (bias) {
-    const Raw8<T> b = load8((const T*)bias, col, p.d);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] += b.get(e);
-  }
+// tanh to a few units in the last place: its series up to x^9 below 0.25, from exp(2 |x|) above
+__device__ __forceinline__ float tanh_f32(float x) {
+  const float y = fabsf(x), y2 = y * y;
+  const float series = y * (1.f + y2 * (-1.f / 3 + y2 * (2.f / 15 + y2 * (-17.f / 315 + y2 * (62.f / 2835)))));
+  const float t = 1.f - 2.f * __builtin_amdgcn_rcpf(__expf(2.f * y) + 1.f);
+  return copysignf(y < 0.25f ? series : t, x);
+}
+__device__ __forceinline__ float activated(float g, int act) {
+  return act == SVDMLP_GATE_SIGMOID ? __builtin_amdgcn_rcpf(1.f + __expf(-g)) : act == SVDMLP_GATE_TANH ? tanh_f32(g) : g;
 }
 
-// TPR threads hold a row, thread t columns 8 (i TPR + t) .. + 7, i < NV: 16 lanes hold a block of 128 columns.
-template <class T, class S, int TPR, int NV>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormP p) {
+// TPR threads hold a row, thread t columns 8 (i TPR + t) .. + 7, i < NV: 16 lanes hold a block of 128 columns.  WHOLE: d is a
+// multiple of 8, so that no vector ends early (the code for one that does costs every thread registers).
+template <class T, class S, int TPR, int NV, bool WHOLE>
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
   constexpr int WAVES = TPR / 64;
   __shared__ float part[4 * WAVES];
   const int t = threadIdx.x % TPR;
-  const int64_t row = (int64_t)blockIdx.x * (TPR < 256 ? 256 / TPR : 1) + threadIdx.x / TPR;
+  const int64_t row = (int64_t)blockIdx.x * (TPR == 64 ? 4 : 1) + threadIdx.x / TPR;
   if (row >= p.rows) return;   // whole waves, and whole workgroups where they meet at a barrier
-  Raw8<T> rb[NV];
+  const int end = WHOLE ? 0x7fffffff : p.d;     // of a row, as far as a vector that begins inside has to know
+  Raw8<T> rb[NV], w[NV], nw[NV];
   Raw8<S> rr[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int col = (i * TPR + t) * 8;
-    rb[i] = p.branch && col < p.d ? load8((const T*)p.branch + row * p.branch_ld, col, p.d) : Raw8<T>{};
-    rr[i] = p.residual && col < p.d ? load8((const S*)p.residual + row * p.residual_ld, col, p.d) : Raw8<S>{};
+    const bool in = col < p.d;
+    rb[i] = p.branch && in ? load8((const T*)p.branch + row * p.branch_ld, col, end) : Raw8<T>{};
+    rr[i] = p.residual && in ? load8((const S*)p.residual + row * p.residual_ld, col, end) : Raw8<S>{};
+    w[i] = p.weight && in ? load8((const T*)p.weight, col, end) : Raw8<T>{};
+    nw[i] = p.next_weight && in ? load8((const T*)p.next_weight, col, end) : Raw8<T>{};
   }
   float v[NV][8];
 #pragma unroll
@@ -98,48 +101,63 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormP p) {
   for (int i = 0; i < NV; ++i) {
     const int col = (i * TPR + t) * 8;
     if (col >= p.d) continue;
-    if (p.kind != SVDMLP_NORM_NONE) affine<T>(v[i], p.weight, p.bias, col, p);
+    if (p.weight) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] *= w[i].get(e) + p.weight_plus;
+    }
+    if (p.bias) {
+      const Raw8<T> b = load8((const T*)p.bias, col, end);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] += b.get(e);
+    }
     if (p.branch_scale) {
-      const Raw8<T> s = load8((const T*)p.branch_scale, col, p.d);
+      const Raw8<T> s = load8((const T*)p.branch_scale, col, end);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] *= s.get(e);
     }
     if (p.gate) {
-      const Raw8<T> s = load8((const T*)p.gate + row / p.gate_rows * p.gate_ld, col, p.d);
+      const Raw8<T> s = load8((const T*)p.gate + row / p.gate_rows * p.gate_ld, col, end);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float g = s.get(e);
-        v[i][e] *= p.gate_act == SVDMLP_GATE_SIGMOID ? 1.f / (1.f + __expf(-g)) : p.gate_act == SVDMLP_GATE_TANH ? tanhf(g) : g;
-      }
+      for (int e = 0; e < 8; ++e) v[i][e] *= activated(s.get(e), p.gate_act);
     }
     if (p.residual) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] += p.residual_scale * rr[i].get(e);
     }
+    if (!WHOLE) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (col + e >= p.d) v[i][e] = 0.f;
-    if (p.h) store8((S*)p.h + row * p.h_ld, col, p.d, v[i]);
+      for (int e = 0; e < 8; ++e)
+        if (col + e >= p.d) v[i][e] = 0.f;
+    }
+    if (p.h) store8((S*)p.h + row * p.h_ld, col, end, v[i]);
   }
   if (p.next_kind == SVDMLP_NORM_NONE) return;
   normalize<TPR, NV>(v, p.next_kind, p.next_eps, p, t, part + 2 * WAVES);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int col = (i * TPR + t) * 8;
-    if (col < p.d) affine<T>(v[i], p.next_weight, p.next_bias, col, p);
+    if (p.next_weight) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] *= nw[i].get(e) + p.weight_plus;
+    }
+    if (p.next_bias && col < p.d) {
+      const Raw8<T> b = load8((const T*)p.next_bias, col, end);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] += b.get(e);
+    }
     if (!p.out_f8) {
-      if (col < p.d) store8((T*)p.out + row * p.out_ld, col, p.d, v[i]);
+      if (col < p.d) store8((T*)p.out + row * p.out_ld, col, end, v[i]);
       continue;
     }
     float amax = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      if (col + e >= p.d) v[i][e] = 0.f;
+      if (!WHOLE && col + e >= p.d) v[i][e] = 0.f;
       amax = fmaxf(amax, fabsf(v[i][e]));
     }
     const __bf16 s = scale_of(max16(amax));
     if (col < p.d) {
-      store_codes8((unsigned char*)p.out + row * p.out_ld, col, p.d, v[i], 1.f / (float)s);
+      store_codes8((unsigned char*)p.out + row * p.out_ld, col, end, v[i], 1.f / (float)s);
       if (t % 16 == 0) p.out_scales[(int64_t)(col / SCALE_BLOCK) * p.out_scales_ld + row] = s;
     }
   }
@@ -147,16 +165,22 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormP p) {
 
 template <class T, class S, int TPR, int NV>
 static void run_norm(const NormP& p, hipStream_t st) {
-  constexpr int per = TPR < 256 ? 256 / TPR : 1;
-  k_norm<T, S, TPR, NV><<<(unsigned)((p.rows + per - 1) / per), TPR < 256 ? 256 : TPR, 0, st>>>(p);
+  constexpr int per = TPR == 64 ? 4 : 1;
+  const unsigned wgs = (unsigned)((p.rows + per - 1) / per);
+  if (p.d % 8 == 0) k_norm<T, S, TPR, NV, true><<<wgs, TPR == 64 ? 256 : TPR, 0, st>>>(p);
+  else k_norm<T, S, TPR, NV, false><<<wgs, TPR == 64 ? 256 : TPR, 0, st>>>(p);
 }
 
 template <class T, class S>
 static void launch_norm(const NormP& p, hipStream_t st) {
+  // As few vectors a thread as a workgroup's size allows: a row's chain (loads, sums over the workgroup, stores) is what a CU has
+  // four of at 512 threads.  us in a graph, 1024 / 512 / 256 / 128 threads for the row: 4096 x 4096 in 8 bits with a residual
+  // 27.6 / 26.3 / 26.3 / 28.5, one such row 5.0 / 4.6 / 4.9, 8192 x 5120 with gate and fp32 residual - / 109 / 113 / 139.
   if (p.d <= 512) run_norm<T, S, 64, 1>(p, st);
   else if (p.d <= 2048) run_norm<T, S, 256, 1>(p, st);
-  else if (p.d <= 4096) run_norm<T, S, 256, 2>(p, st);
-  else if (p.d <= 8192) run_norm<T, S, 256, 4>(p, st);
+  else if (p.d <= 4096) run_norm<T, S, 512, 1>(p, st);
+  else if (p.d <= 8192) run_norm<T, S, 512, 2>(p, st);
+  else if (p.d <= 16384) run_norm<T, S, 512, 4>(p, st);
   else run_norm<T, S, 1024, 4>(p, st);
 }
 

@@ -190,8 +190,8 @@ def test_a_call_on_another_device_makes_it_current(monkeypatch):
     now, seen = [0], []
 
     class on:
-        def __init__(self, device):
-            self.index = device.index
+        def __init__(self, index):
+            self.index = index
 
         def __enter__(self):
             self.before, now[0] = now[0], self.index
@@ -199,13 +199,13 @@ def test_a_call_on_another_device_makes_it_current(monkeypatch):
         def __exit__(self, *e):
             now[0] = self.before
 
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(B, "_current_device", lambda: now[0])
     monkeypatch.setattr(torch.cuda, "device", on)
     monkeypatch.setattr(B, "_current_raw_stream", lambda index: 100 + index)
     monkeypatch.setattr(B, "lib", lambda: types.SimpleNamespace(op=lambda args, stream: seen.append((now[0], stream)) or 0))
-    B._run("op", 1, b"", torch.device("cuda", 1), None)
-    B._run("op", 1, b"", torch.device("cuda", 0), None)
-    B._run("op", 1, b"", torch.device("cuda", 1), types.SimpleNamespace(cuda_stream=7))
+    B._run("op", 1, b"", 1, None)
+    B._run("op", 1, b"", 0, None)
+    B._run("op", 1, b"", 1, types.SimpleNamespace(cuda_stream=7))
     assert seen == [(1, 101), (0, 100), (1, 7)] and now == [0]
 
 
