@@ -238,11 +238,11 @@ __device__ __forceinline__ void mm_result(const MmP& p, const f32x4 (&acc)[NT][M
 }
 
 // ---- tiles through LDS ------------------------------------------------------------------------------
-// Four times 16 bytes a lane, global -> LDS, if t < steps: a wave-uniform base and a 32-bit offset per lane; lane l lands at
+// C times 16 bytes a lane, global -> LDS, if t < steps: a wave-uniform base and a 32-bit offset per lane; lane l lands at
 // lds_dst + 16 l, each copy STRIDE bytes after the one before.  The branch is inside so that the compiler sees none in the
 // middle of a step, where it would move registers about.
 template <int STRIDE>
-__device__ __forceinline__ void copy4(const char* sbase, const unsigned (&v)[4], unsigned lds_dst, int t, int steps) {
+__device__ __forceinline__ void copies(const char* sbase, const unsigned (&v)[4], unsigned lds_dst, int t, int steps) {
   asm volatile(
       "s_cmp_ge_i32 %6, %7\n\ts_cbranch_scc1 .Lskip%=\n\t"
       "s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0\n\t"
@@ -252,6 +252,14 @@ __device__ __forceinline__ void copy4(const char* sbase, const unsigned (&v)[4],
       ".Lskip%=:" ::"s"(sbase), "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "s"(lds_dst), "s"(t), "s"(steps), "n"(STRIDE)
       : "memory", "m0", "scc");
 }
+template <int STRIDE>
+__device__ __forceinline__ void copies(const char* sbase, const unsigned (&v)[2], unsigned lds_dst, int t, int steps) {
+  asm volatile(
+      "s_cmp_ge_i32 %4, %5\n\ts_cbranch_scc1 .Lskip%=\n\t"
+      "s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0\n\t"
+      "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %0\n"
+      ".Lskip%=:" ::"s"(sbase), "v"(v[0]), "v"(v[1]), "s"(lds_dst), "s"(t), "s"(steps), "n"(STRIDE) : "memory", "m0", "scc");
+}
 
 // Waits until at most N of this wave's copies are on their way, or none unless t < steps.
 template <int N>
@@ -260,37 +268,36 @@ __device__ __forceinline__ void wait_copies(int t, int steps) {
                ::"s"(t), "s"(steps), "n"(N) : "memory", "scc");
 }
 
-// 2 x WN waves, each with 16 MT rows x 16 NT columns.  A step is one block of the contraction: the tile's rows of W and of A,
+// WM x WN waves, each with 16 MT rows x 16 NT columns.  A step is one block of the contraction: the tile's rows of A and of W,
 // 128 bytes each, lie in LDS row by row, the eight 16-byte pieces of row r in the order piece ^ (r % 8), which spreads the
 // reads of sixteen rows over the banks.  A wave reads its rows of W into registers first, then its rows of A tile by tile.
 //
-// The two halves of the workgroup (rows 0 .. ROWS / 2 - 1 and the others) run half a step apart, with a barrier every half
-// step, so that of the two waves of a SIMD (256 x 256 tile) one is in the middle of its products while the other one waits
+// The two halves of the workgroup (the upper rows of the tile and the lower) run half a step apart, with a barrier every half
+// step, so that of the two waves of a SIMD (eight waves) one is in the middle of its products while the other one waits
 // for its first reads.  Half h starts step t in phase 2 t + h.  It then copies its rows of A of step t + 1 (two buffers: it
 // has read those of step t - 1 itself) and its share of the rows of W of step t + 2 (three buffers: the second half read those
 // of step t - 1 in phase 2 t - 1).  Before a step it waits for its A, in the middle of one for its share of the next W,
 // which the first half reads in the next phase.
-template <int MT, int NT, int WN>
+template <int MT, int NT, int WM, int WN>
 struct MmTile {
-  static constexpr int ROWS = 32 * MT, WAVES = 2 * WN;     // of the tile, and columns
-  static_assert(16 * NT * WN == ROWS && ROWS == 32 * WAVES, "units of equal size, four copies a wave");
-  static constexpr int UNIT = ROWS * SCALE_BLOCK;                // rows of A or W of a step
-  static constexpr int W_AT = 2 * UNIT;                          // two units for A, then three for W
-  static constexpr int LDS = 5 * UNIT;
+  static constexpr int TM = 16 * MT * WM, TN = 16 * NT * WN, WAVES = WM * WN, HALF = WAVES / 2;
+  static constexpr int CA = TM / 8 / WAVES, CW = TN / 8 / WAVES;      // copies of a wave per step, eight rows each
+  static constexpr int A_UNIT = TM * SCALE_BLOCK, W_UNIT = TN * SCALE_BLOCK;      // rows of a step
+  static constexpr int W_AT = 2 * A_UNIT, LDS = W_AT + 3 * W_UNIT;
   static_assert(WAVES * MmResult<MT, NT>::BYTES <= LDS, "the result passes through the same memory");
 };
 
-template <int MT, int NT, int WN>
-__global__ __launch_bounds__(128 * WN) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_mm_tile(MmP p) {
-  using T = MmTile<MT, NT, WN>;
+template <int MT, int NT, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_mm_tile(MmP p) {
+  using T = MmTile<MT, NT, WM, WN>;
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / WN, wn = wave % WN;
-  const int mtiles = (p.M + T::ROWS - 1) / T::ROWS, ntiles = (p.N + T::ROWS - 1) / T::ROWS;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / WN, wn = wave % WN, half = wave / T::HALF;
+  const int mtiles = (p.M + T::TM - 1) / T::TM, ntiles = (p.N + T::TN - 1) / T::TN;
   int mt, nt;
   banded_tile(xcd_contiguous_id(blockIdx.x, gridDim.x), mtiles, ntiles, p.band, mt, nt);
   // divisions are done by the vector unit; copies take their addresses from scalar registers
-  const int m0 = __builtin_amdgcn_readfirstlane(mt) * T::ROWS, n0 = __builtin_amdgcn_readfirstlane(nt) * T::ROWS;
+  const int m0 = __builtin_amdgcn_readfirstlane(mt) * T::TM, n0 = __builtin_amdgcn_readfirstlane(nt) * T::TN;
   const unsigned lds0 = lds_offset_of(lds);
   // A block that ends inside comes first, so that only the prologue has to clear what lies behind it.
   const int steps = p.KB, tail = p.K % SCALE_BLOCK;
@@ -302,18 +309,17 @@ __global__ __launch_bounds__(128 * WN) __attribute__((amdgpu_waves_per_eu(2, 2))
   // copies: lane l brings piece (l % 8) ^ (l / 8) of row l / 8 of eight rows; rows beyond the matrix repeat its last one
   const int cr = lane / 8, cp = (lane % 8) ^ cr;
   const char *abase = p.a + m0 * p.a_ld, *wbase = p.w + n0 * p.w_ld;
-  unsigned aoff[4], woff[4];
-  const int a8 = wm * (T::ROWS / 16) + wn;       // eight rows of A: a8 + WN c, in this wave's half; of W: wave + WAVES c
+  unsigned aoff[T::CA], woff[T::CW];
+  const int a8 = half * (T::TM / 16) + wave % T::HALF;       // eight rows of A: a8 + HALF c, of this wave's half; of W: wave + WAVES c
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    aoff[c] = (unsigned)min(arow_of(8 * (a8 + WN * c) + cr), p.M - 1 - m0) * (unsigned)p.a_ld + 16 * cp;
-    woff[c] = (unsigned)min(8 * (wave + T::WAVES * c) + cr, p.N - 1 - n0) * (unsigned)p.w_ld + 16 * cp;
-  }
-  auto issue_a = [&](const unsigned (&off)[4], int t, int unit) {
-    copy4<1024 * WN>(abase + (int64_t)block_of(t) * SCALE_BLOCK, off, lds0 + unit * T::UNIT + 1024 * a8, t, steps);
+  for (int c = 0; c < T::CA; ++c) aoff[c] = (unsigned)min(arow_of(8 * (a8 + T::HALF * c) + cr), p.M - 1 - m0) * (unsigned)p.a_ld + 16 * cp;
+#pragma unroll
+  for (int c = 0; c < T::CW; ++c) woff[c] = (unsigned)min(8 * (wave + T::WAVES * c) + cr, p.N - 1 - n0) * (unsigned)p.w_ld + 16 * cp;
+  auto issue_a = [&](const unsigned (&off)[T::CA], int t, int unit) {
+    copies<1024 * T::HALF>(abase + (int64_t)block_of(t) * SCALE_BLOCK, off, lds0 + unit * T::A_UNIT + 1024 * a8, t, steps);
   };
-  auto issue_w = [&](const unsigned (&off)[4], int t, int unit) {
-    copy4<1024 * T::WAVES>(wbase + (int64_t)block_of(t) * SCALE_BLOCK, off, lds0 + T::W_AT + unit * T::UNIT + 1024 * wave, t, steps);
+  auto issue_w = [&](const unsigned (&off)[T::CW], int t, int unit) {
+    copies<1024 * T::WAVES>(wbase + (int64_t)block_of(t) * SCALE_BLOCK, off, lds0 + T::W_AT + unit * T::W_UNIT + 1024 * wave, t, steps);
   };
   auto clear8 = [&](int at) {      // what this lane brought beyond the end of the contraction
     u32x4* q = (u32x4*)(lds + at + lane * 16);
@@ -371,27 +377,28 @@ __global__ __launch_bounds__(128 * WN) __attribute__((amdgpu_waves_per_eu(2, 2))
   } else {
     // how far this lane's piece lies behind the last one that holds codes
     const unsigned back = (unsigned)max(0, 16 * cp - ((tail - 1) & ~15));
-    const unsigned wv[4] = {woff[0] - back, woff[1] - back, woff[2] - back, woff[3] - back};
-    const unsigned av[4] = {aoff[0] - back, aoff[1] - back, aoff[2] - back, aoff[3] - back};
+    unsigned av[T::CA], wv[T::CW];
+#pragma unroll
+    for (int c = 0; c < T::CA; ++c) av[c] = aoff[c] - back;
+#pragma unroll
+    for (int c = 0; c < T::CW; ++c) wv[c] = woff[c] - back;
     issue_w(wv, 0, 0);
     issue_a(av, 0, 0);
     wait_vmcnt<0>();
-    for (int c = 0; c < 4; ++c) {
-      clear8(1024 * (a8 + WN * c));
-      clear8(T::W_AT + 1024 * (wave + T::WAVES * c));
-    }
+    for (int c = 0; c < T::CA; ++c) clear8(1024 * (a8 + T::HALF * c));
+    for (int c = 0; c < T::CW; ++c) clear8(T::W_AT + 1024 * (wave + T::WAVES * c));
   }
   issue_w(woff, 1, 1);
-  if (wm == 1) {       // half a step behind
-    wait_copies<4>(1, steps);
+  if (half == 1) {     // half a step behind
+    wait_copies<T::CW>(1, steps);
     __builtin_amdgcn_s_waitcnt(0xC07F);
     lds_barrier();
   }
   int wu = 0;          // unit of the step's rows of W
   for (int t = 0; t < steps; ++t) {
-    const int at_a = t % 2 * T::UNIT, at_w = T::W_AT + wu * T::UNIT;
+    const int at_a = t % 2 * T::A_UNIT, at_w = T::W_AT + wu * T::W_UNIT;
     // this wave's copies of the step's A have landed, its LDS accesses are done
-    wait_copies<4>(t + 1, steps);
+    wait_copies<T::CW>(t + 1, steps);
     __builtin_amdgcn_s_waitcnt(0xC07F);
     lds_barrier();
     float s[MT];
@@ -408,7 +415,7 @@ __global__ __launch_bounds__(128 * WN) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       if (i == MT / 2) {
-        wait_copies<8>(t + 2, steps);
+        wait_copies<T::CA + T::CW>(t + 2, steps);
         lds_barrier();
       }
       if (i + 1 < MT) fa[(i + 1) % 2] = frag(at_a, arow + 16 * (i + 1));
@@ -426,7 +433,7 @@ __global__ __launch_bounds__(128 * WN) __attribute__((amdgpu_waves_per_eu(2, 2))
     s_last = s[MT - 1];
     wu = wu < 2 ? wu + 1 : 0;
   }
-  if (wm == 0) lds_barrier();      // as many as the other half
+  if (half == 0) lds_barrier();    // as many as the other half
 #pragma unroll
   for (int q = Q - LAG; q < Q; ++q) add(q, s_last);
 
@@ -612,28 +619,31 @@ __global__ __launch_bounds__(256) void k_mm_join(MmP p) {
 
 // ---- host -------------------------------------------------------------------------------------------
 // Which kernel, and into how many ranges the contraction is cut: the least time by a model of the compute units.  A
-// workgroup's steps take `step` us where it has a CU to itself (its own chain of waits), `share` us each where `per_cu` of them
-// share one (the CU's copies and matrix products), a tile besides `tile` us for its first copies and its result, a launch
-// LAUNCH_US; cut contractions and 8-bit results of 64-column tiles add a second launch that reads the partial sums.  The figures
-// are fitted to launches in a graph; model / measured us of the kernel chosen and the next best, rows x contraction x columns:
-//   16 x 4096 x 14336     ring 32x64 11.2 / 11.3, few 14.6 / 13.5        128 x 2048 x 8192  ring 32x64 8.7 / 8.7, ring 64x64 8.6 / 8.9
-//   256 x 4096 x 4096     ring 64x64 14.0 / 13.9, ring 64x128 18.0 / 18.3  1024 x 4096 x 4096  ring 64x128 26.9 / 25.6, tile 128 29.5 / 27.8
-//   512 x 4096 x 14336    tile 128 43 / 38, ring 64x128 51 / 45          4096 x 8192 x 16384 tile 256 462 / 437, tile 128 630 / 590
-enum { MM_FEW = 0, MM_RING_32, MM_RING_64, MM_RING_64_128, MM_TILE_128, MM_TILE_256, MM_KINDS };
+// workgroup's steps take `step` us where it has a CU to itself (its own chain of waits), `pair` where it shares it with another,
+// `share` each where more do (the CU's copies and matrix products; below one a CU, the chip's share of them), a tile besides
+// `tile` us for its first copies and its result, a launch LAUNCH_US; cut contractions and 8-bit results of 64-column tiles add
+// a second launch that reads the partial sums.  The figures are fitted to launches in a graph.  Over 7400 sizes of 1 - 8192 rows,
+// 100 - 16384 columns and contractions, times the chosen kernel took over those of the fastest: 1.013 in the geometric mean,
+// 1.40 at most.  Model / measured us of the chosen and of others, rows x contraction x columns:
+//   16 x 4096 x 14336   ring 32x64 11.2 / 11.3, few 14.6 / 12.7       256 x 4096 x 4096    ring 64x64 14.0 / 13.9, ring 64x128 18 / 18
+//   1024 x 4096 x 4096  ring 64x128 26.9 / 28.7, tile 128x256 34 / 32   2048 x 4096 x 4096   tile 128x256 38 / 37, tile 256x256 52 / 47
+//   4096 x 4096 x 4096  tile 256x256 61 / 61, tile 128x256 74 / 71     4096 x 8192 x 16384  tile 256x256 449 / 440, tile 128x256 529 / 579
+// (Further tiles measured and not kept: 128 x 128 with four waves, 256 x 128, 128 x 64, 32 x 128: level or behind one of these.)
+enum { MM_FEW = 0, MM_RING_32, MM_RING_64, MM_RING_64_128, MM_TILE_128_256, MM_TILE_256, MM_KINDS };
 struct MmKind {
   const char* name;
   int rows, cols, max_rows;      // of a tile; rows of A that it takes (0: any)
-  double step, share, tile;
+  double step, pair, share, tile;
 };
 constexpr MmKind MM_KIND[MM_KINDS] = {
-    {"k_mm_few[tile=16x16", 16, 16, 16, 0.62 / FEW_WAVES, 0.60 / FEW_WAVES, 0.},
-    {"k_mm_ring[tile=32x64", 32, 64, 0, 0.26, 0.17, 0.4},
-    {"k_mm_ring[tile=64x64", 64, 64, 0, 0.34, 0.235, 0.6},
-    {"k_mm_ring[tile=64x128", 64, 128, 0, 0.45, 0.35, 1.0},
-    {"k_mm_tile[tile=128x128", 128, 128, 0, 0.775, 0.57, 2.2},
-    {"k_mm_tile[tile=256x256", 256, 256, 0, 1.7, 1.7, 6.0},
+    {"k_mm_few[tile=16x16", 16, 16, 16, 0.62 / FEW_WAVES, 1.20 / FEW_WAVES, 0.60 / FEW_WAVES, 0.},
+    {"k_mm_ring[tile=32x64", 32, 64, 0, 0.26, 0.34, 0.17, 0.4},
+    {"k_mm_ring[tile=64x64", 64, 64, 0, 0.34, 0.40, 0.255, 0.6},
+    {"k_mm_ring[tile=64x128", 64, 128, 0, 0.45, 0.70, 0.36, 1.0},
+    {"k_mm_tile[tile=128x256", 128, 256, 0, 0.87, 2.0, 1.0, 3.5},
+    {"k_mm_tile[tile=256x256", 256, 256, 0, 1.35, 3.3, 1.65, 6.0},
 };
-constexpr double LAUNCH_US = 2.5, JOIN_US = 2.3, HBM_BYTES_PER_US = 6.8e6, PART_BYTES_PER_US = 4.0e6;
+constexpr double LAUNCH_US = 2.5, JOIN_US = 2.3, JOIN_RANGE_US = 0.1, HBM_BYTES_PER_US = 6.8e6, PART_BYTES_PER_US = 4.0e6;
 constexpr int MM_CUS = 256;      // the model's device, so that a result's order of sums goes by the extents alone
 
 struct MmPlan {
@@ -653,7 +663,7 @@ static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, MmPlan* best) 
     const MmKind& kind = MM_KIND[k];
     if (kind.max_rows && M > kind.max_rows) continue;
     const int64_t tiles = ((M + kind.rows - 1) / kind.rows) * ((N + kind.cols - 1) / kind.cols);
-    for (int r = 1; r <= (k < MM_TILE_128 ? 32 : 1) && r <= KB; r *= 2) {     // the tile kernels take whole contractions
+    for (int r = 1; r <= (k < MM_TILE_128_256 ? 32 : 1) && r <= KB; r *= 2) {     // the tile kernels take whole contractions
       MmPlan q;
       q.kind = k;
       q.tiles = tiles;
@@ -662,18 +672,23 @@ static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, MmPlan* best) 
       if (q.ranges != r && r > 1) continue;
       if (tiles * r >= int64_t(1) << 22) continue;        // a grid of 512 lanes each, below 2^31
       q.join = r > 1 || (out_type == SVDMLP_F8 && kind.cols < SCALE_BLOCK);
-      const double per_cu = (double)((tiles * r + MM_CUS - 1) / MM_CUS);
-      double step = kind.step, share = kind.share;
+      const int64_t per_cu = (tiles * r + MM_CUS - 1) / MM_CUS;
+      const bool on_lines = k == MM_FEW || (K + 15) / 16 % 8 == 0;     // packed rows begin on lines; else 128 bytes take two
+      double step = per_cu < 2 ? kind.share * tiles * r / MM_CUS : per_cu == 2 && on_lines ? kind.pair : kind.share * per_cu;
+      if (step < kind.step) step = kind.step;
       int steps = q.range_blocks;
-      if (k == MM_FEW) {       // eight waves take a block each; every workgroup reads the rows of A
+      double hbm = ((double)N * K + (double)M * K + (double)M * N * (out_type == SVDMLP_F8 ? 1 : 2)) / HBM_BYTES_PER_US;
+      if (k == MM_FEW) {          // eight waves take a block each; every workgroup reads the rows of A
         steps = (steps + FEW_WAVES - 1) / FEW_WAVES * FEW_WAVES;
-        step += 0.022 / FEW_WAVES * M;
-        share += 0.022 / FEW_WAVES * M;
+        step += 0.022 / FEW_WAVES * M * per_cu;
       }
-      double t = kind.tile * per_cu + steps * (step > share * per_cu ? step : share * per_cu);
-      const double bytes = (double)N * K + (double)M * K + (double)M * N * (out_type == SVDMLP_F8 ? 1 : 2);
-      if (t < bytes / HBM_BYTES_PER_US) t = bytes / HBM_BYTES_PER_US;
-      q.est_us = LAUNCH_US + t + (q.join ? JOIN_US + 8. * M * N * r / PART_BYTES_PER_US : 0.);
+      if (!on_lines) {
+        step *= k == MM_TILE_256 ? 1.05 : 1.25;
+        hbm *= 1.3;
+      }
+      double t = kind.tile * per_cu + steps * step;
+      if (t < hbm) t = hbm;
+      q.est_us = LAUNCH_US + t + (q.join ? JOIN_US + JOIN_RANGE_US * r + 8. * M * N * r / PART_BYTES_PER_US : 0.);
       if (best->kind < 0 || q.est_us < best->est_us) *best = q;
     }
   }
@@ -686,7 +701,8 @@ static void launch_join(const MmP& p, hipStream_t st) {
   const unsigned wgs = (unsigned)((p.M + 15) / 16 * scale_blocks(p.N));
   if (p.ranges == 1) k_mm_join<1><<<wgs, 256, 0, st>>>(p);
   else if (p.ranges <= 4) k_mm_join<4><<<wgs, 256, 0, st>>>(p);
-  else k_mm_join<8><<<wgs, 256, 0, st>>>(p);
+  else if (p.ranges <= 8) k_mm_join<8><<<wgs, 256, 0, st>>>(p);
+  else k_mm_join<16><<<wgs, 256, 0, st>>>(p);
 }
 
 static void launch_mm(MmP& p, const MmPlan& q, hipStream_t st) {
@@ -697,8 +713,8 @@ static void launch_mm(MmP& p, const MmPlan& q, hipStream_t st) {
     case MM_RING_32: k_mm_ring<1, 2><<<wgs, 256, 0, st>>>(p); break;
     case MM_RING_64: k_mm_ring<2, 2><<<wgs, 256, 0, st>>>(p); break;
     case MM_RING_64_128: k_mm_ring<2, 4><<<wgs, 256, 0, st>>>(p); break;
-    case MM_TILE_128: k_mm_tile<4, 4, 2><<<wgs, 256, 0, st>>>(p); break;
-    default: k_mm_tile<8, 4, 4><<<wgs, 512, 0, st>>>(p); break;
+    case MM_TILE_128_256: k_mm_tile<4, 4, 2, 4><<<wgs, 512, 0, st>>>(p); break;
+    default: k_mm_tile<8, 4, 2, 4><<<wgs, 512, 0, st>>>(p); break;
   }
 }
 

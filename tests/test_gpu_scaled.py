@@ -126,7 +126,7 @@ MATMULS = [
     # what else the product's kernels and their cuts of the contraction are chosen for (a host test sees to it that all are here)
     (3, 6000, 300), (700, 500, 1300), (520, 300, 2500), (700, 4100, 400), (90, 1100, 4000), (2741, 2252, 135), (1301, 4999, 300),
     (1290, 5000, 513), (300, 2600, 6000), (2100, 5000, 257), (2111, 4983, 600), (1500, 600, 9000), (3, 66, 555), (284, 1738, 1842),
-    (2732, 331, 61), (353, 131, 4010), (2071, 905, 3518),
+    (2732, 331, 61), (353, 131, 4010), (2071, 905, 3518), (3585, 2000, 72), (3585, 2830, 120), (2747, 1472, 256),
 ]
 
 
