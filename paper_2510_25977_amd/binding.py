@@ -406,7 +406,7 @@ def _codes(t, what: str, shape, device: int):
     ptr, ld = _rows(codes, what, shape, _F8, device, 16)
     rows = shape[0]
     sptr, sld = _rows(scales, "the scales of " + what, ((shape[1] + SCALE_BLOCK - 1) // SCALE_BLOCK, rows), _BF16, device)
-    return ptr, ld, sptr, sld if sld > rows else rows
+    return ptr, ld, sptr, sld
 
 
 def _weight_codes(t, what: str, shape, device: int):

@@ -184,6 +184,27 @@ def test_the_binding_checks_tensors(monkeypatch):
         B.SvdMlpF8(Ug=fake(256, 64), Vg=fake(65, 512), kind=B.SVDMLP_LINEAR)
 
 
+def test_scales_that_a_stride_repeats_are_refused(monkeypatch):
+    """Scales [blocks, rows] whose blocks lie less than `rows` apart (one per row, expanded over the blocks; a buffer of fewer
+    rows seen through strides) are not what the kernels read: their stride reaches the C entry, which refuses it."""
+    monkeypatch.setattr(B, "_current_device", lambda: -1)
+    monkeypatch.setattr(B, "_current_raw_stream", lambda index: 0)
+    good = B.empty_scaled(4, 256, "cpu")
+    codes = good.codes.as_subclass(_OnDevice)
+    per_row = torch.zeros(1, 4, dtype=torch.bfloat16).expand(2, 4)
+    weights = B.empty_scaled(64, 256, "cpu", 128)
+    out = torch.empty(4, 64, dtype=torch.bfloat16)
+    for scales in (per_row, torch.zeros(7, dtype=torch.bfloat16).as_strided((2, 4), (3, 1))):
+        with pytest.raises(B.SvdMlpError) as e:
+            B.scaled_matmul((codes, scales), weights, out=out)
+        assert e.value.status == B.SVDMLP_INVALID_ARGUMENT
+        with pytest.raises(B.SvdMlpError):
+            B.quantize(fake(4, 256), out=(good.codes, scales))
+        with pytest.raises(B.SvdMlpError):
+            B.norm_in(fake(4, 256), out=(good.codes, scales))
+    assert B._codes((good.codes[:1], good.scales[:, 1:2]), "a", (1, 256), -1)[3] == 4      # one row of many: a stride as any
+
+
 def test_a_call_on_another_device_makes_it_current(monkeypatch):
     """Kernels go to the current device, so an operator whose tensors lie elsewhere switches to theirs and back, and asks for
     the current stream of that device."""
