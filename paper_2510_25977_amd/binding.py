@@ -429,10 +429,20 @@ def _device_of(t: torch.Tensor, what: str) -> int:
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _run(name: str, rows: int, args: bytes, device: int, stream) -> None:
+def _on(stream: torch.cuda.Stream, op, t, *args, **kw):
+    """op(t, ...) with its launches on `stream`, and the results and workspaces that it makes `stream`'s as well: memory of the
+    current stream may be freed memory that work on that stream still uses."""
+    device = (t[0] if isinstance(t, tuple) else t).get_device()
+    if stream.device_index != device:
+        raise ValueError(f"the stream is one of cuda:{stream.device_index}, the tensors are on cuda:{device}")
+    with torch.cuda.stream(stream):
+        return op(t, *args, **kw)
+
+
+def _run(name: str, rows: int, args: bytes, device: int) -> None:
     if rows == 0:            # a tensor of no rows has no address
         return
-    s = _current_raw_stream(device) if stream is None else stream.cuda_stream
+    s = _current_raw_stream(device)
     if device != _current_device():          # kernels are launched on the current device
         with torch.cuda.device(device):
             st = getattr(lib(), name)(args, s)
@@ -446,6 +456,8 @@ def quantize(x: torch.Tensor, gate_with: Optional[torch.Tensor] = None, *, block
              stream: Optional[torch.cuda.Stream] = None) -> Scaled:
     """x, or SiLU(x) * gate_with, as e4m3 codes with a scale per row and 128 columns (``block_rows=128``: weights, one per
     128 x 128).  x: [R, C] bfloat16 or float32."""
+    if stream is not None:
+        return _on(stream, quantize, x, gate_with, block_rows=block_rows, out=out)
     dev, shape, dtype = _device_of(x, "x"), x.shape, x.dtype
     if dtype not in _TORCH_DTYPE:
         raise ValueError("x must be bfloat16 or float32")
@@ -458,13 +470,13 @@ def quantize(x: torch.Tensor, gate_with: Optional[torch.Tensor] = None, *, block
         cp, cld, sp, sld = _codes(out, "out", shape, dev)
     else:
         (cp, cld, sp), sld = _weight_codes(out, "out", shape, dev), 0
-    _run("svdmlp_quantize", R, QUANTIZE_ARGS.pack(R, C, _TORCH_DTYPE[dtype], block_rows, xp, gp, xld, gld, cp, sp, cld, sld), dev, stream)
+    _run("svdmlp_quantize", R, QUANTIZE_ARGS.pack(R, C, _TORCH_DTYPE[dtype], block_rows, xp, gp, xld, gld, cp, sp, cld, sld), dev)
     return Scaled(*out)
 
 
-def _norm(branch, residual, weight, bias, kind, eps, weight_plus, residual_scale, branch_scale, gate, gate_rows, gate_act,
-          next_weight, next_bias, next_kind, next_eps, h, out, scaled, want_h, stream):
-    x = residual if residual is not None else branch      # of the residual stream's type
+def _norm(x, branch, residual, weight, bias, kind, eps, weight_plus, residual_scale, branch_scale, gate, gate_rows, gate_act,
+          next_weight, next_bias, next_kind, next_eps, h, out, scaled, want_h):
+    """x: the residual, or the branch where there is none: of the residual stream's type"""
     dev, shape, stream_dtype = _device_of(x, "x"), x.shape, x.dtype
     M, d = shape
     # the type of everything but the residual stream
@@ -498,7 +510,7 @@ def _norm(branch, residual, weight, bias, kind, eps, weight_plus, residual_scale
         weight_plus, residual_scale, rp, bp, rld, bld, _vector(weight, "weight", d, dtype, dev), _vector(bias, "bias", d, dtype, dev),
         _vector(branch_scale, "branch_scale", d, dtype, dev), gp, gld, _vector(next_weight, "next_weight", d, dtype, dev),
         _vector(next_bias, "next_bias", d, dtype, dev), hp, hld, op, old, sp, sld)
-    _run("svdmlp_norm", M, args, dev, stream)
+    _run("svdmlp_norm", M, args, dev)
     return h, out
 
 
@@ -509,8 +521,9 @@ def norm_in(x: torch.Tensor, weight: Optional[torch.Tensor] = None, *, bias: Opt
     """The norm before a block: norm(residual_scale * x + add) * (weight + weight_plus) + bias, as a tensor of the weights'
     type or, with ``scaled`` (or a ``Scaled`` as ``out``), in 8 bits.  x is the residual stream, float32 or of the weights'
     type; ``add`` what the block before adds to it; the sum goes to ``h`` if that is given (x itself is allowed)."""
-    return _norm(add, x, None, None, NORM_NONE, eps, weight_plus, residual_scale, None, None, 1, GATE_PLAIN, weight, bias, kind,
-                 eps, h, out, scaled, False, stream)[1]
+    args = (x, add, x, None, None, NORM_NONE, eps, weight_plus, residual_scale, None, None, 1, GATE_PLAIN, weight, bias, kind, eps, h,
+            out, scaled, False)
+    return (_norm(*args) if stream is None else _on(stream, _norm, *args))[1]
 
 
 def norm_out(branch: torch.Tensor, residual: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None, *,
@@ -525,8 +538,10 @@ def norm_out(branch: torch.Tensor, residual: Optional[torch.Tensor] = None, weig
     if next_kind is None:
         wanted = out is not None or scaled or next_weight is not None or next_bias is not None
         next_kind = NORM_RMS if wanted else NORM_NONE
-    return _norm(branch, residual, weight, bias, kind, eps, weight_plus, residual_scale, branch_scale, gate, gate_rows, gate_act,
-                 next_weight, next_bias, next_kind, eps if next_eps is None else next_eps, h, out, scaled, True, stream)
+    args = (branch if residual is None else residual, branch, residual, weight, bias, kind, eps, weight_plus, residual_scale,
+            branch_scale, gate, gate_rows, gate_act, next_weight, next_bias, next_kind, eps if next_eps is None else next_eps, h, out,
+            scaled, True)
+    return _norm(*args) if stream is None else _on(stream, _norm, *args)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -544,6 +559,8 @@ def scaled_matmul(a, w, *, out=None, out_dtype: torch.dtype = torch.bfloat16, st
     """a [M, K] times the transpose of w [N, K], both ``Scaled`` (or pairs of codes and scales): activations with a scale per
     row and 128 columns, weights with one per 128 x 128.  The result [M, N] is ``out`` or a new tensor of ``out_dtype``;
     torch.float8_e4m3fn (or a ``Scaled`` as ``out``) makes it the next product's activations."""
+    if stream is not None:
+        return _on(stream, scaled_matmul, tuple(a), w, out=out, out_dtype=out_dtype)
     codes = a[0]
     dev, shape = _device_of(codes, "a"), codes.shape
     M, K = shape
@@ -565,14 +582,10 @@ def scaled_matmul(a, w, *, out=None, out_dtype: torch.dtype = torch.bfloat16, st
         cp, cld = _rows(out, "out", (M, N), _BF16, dev)
     need, ws = svdmlp_scaled_matmul_workspace_bytes(M, N, K, out_type), 0
     if need:
-        if stream is None:
-            space = torch.empty(need, dtype=torch.uint8, device=codes.device)
-        else:                        # of the stream that uses it, so that it is not handed out again too early
-            with torch.cuda.stream(stream):
-                space = torch.empty(need, dtype=torch.uint8, device=codes.device)
+        space = torch.empty(need, dtype=torch.uint8, device=codes.device)
         ws = space.data_ptr()
     _run("svdmlp_scaled_matmul", M, SCALED_MATMUL_ARGS.pack(M, N, K, out_type, 0, ap, asp, ald, asld, wp, wsp, wld, cp, csp, cld, csld,
-                                                            ws, need), dev, stream)
+                                                            ws, need), dev)
     return out
 
 
@@ -621,9 +634,8 @@ class SvdMlpF8:
 
     def forward(self, X, out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """X: [M, d] bfloat16 or float32, or ``Scaled`` as ``norm_in`` makes it.  The result is ``out`` or a new tensor."""
-        if stream is not None:       # everything in between belongs to that stream
-            with torch.cuda.stream(stream):
-                return self.forward(X, out)
+        if stream is not None:
+            return _on(stream, self.forward, X, out)
         if not isinstance(X, tuple):
             X = quantize(X)
         T = scaled_matmul(X, self.first, out_dtype=_F8)

@@ -474,9 +474,11 @@ def test_a_block_on_a_side_stream_and_in_a_graph(M):
         got = block(inputs[0], mlp, *w)
     side.synchronize()
     assert same(got, 0)
-    y = mlp(B.norm_in(inputs[1], w[0], scaled=True), stream=side)
+    n = B.norm_in(inputs[1], w[0], scaled=True, stream=side)
+    y = mlp(n, stream=side)
+    t = B.scaled_matmul(B.quantize(inputs[2], stream=side), mlp.first, stream=side)
     side.synchronize()
-    torch.cuda.synchronize()
+    assert torch.equal(t, B.scaled_matmul(B.quantize(inputs[2]), mlp.first))
     assert torch.equal(y, mlp(B.norm_in(inputs[1], w[0], scaled=True)))
     x = inputs[0].clone()
     graph = torch.cuda.CUDAGraph()

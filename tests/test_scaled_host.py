@@ -224,10 +224,47 @@ def test_a_call_on_another_device_makes_it_current(monkeypatch):
     monkeypatch.setattr(torch.cuda, "device", on)
     monkeypatch.setattr(B, "_current_raw_stream", lambda index: 100 + index)
     monkeypatch.setattr(B, "lib", lambda: types.SimpleNamespace(op=lambda args, stream: seen.append((now[0], stream)) or 0))
-    B._run("op", 1, b"", 1, None)
-    B._run("op", 1, b"", 0, None)
-    B._run("op", 1, b"", 1, types.SimpleNamespace(cuda_stream=7))
-    assert seen == [(1, 101), (0, 100), (1, 7)] and now == [0]
+    B._run("op", 1, b"", 1)
+    B._run("op", 1, b"", 0)
+    assert seen == [(1, 101), (0, 100)] and now == [0]
+
+
+def test_what_a_call_on_a_stream_makes_is_that_streams(monkeypatch):
+    """Results and workspaces are allocated while the given stream is the current one; one of another device is refused."""
+    current, made = [None], []
+
+    class on:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            current[0] = self.stream
+
+        def __exit__(self, *e):
+            current[0] = None
+
+    empty = torch.empty
+
+    def seen_empty(*args, **kw):
+        made.append(current[0])
+        return empty(*args, **kw)
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch, "empty", seen_empty)
+    monkeypatch.setattr(B, "_run", lambda *a: made.append(current[0]))
+    a, w = B.empty_scaled(8, 4096, "cpu"), B.empty_scaled(4096, 4096, "cpu", 128)
+    a = (a.codes.as_subclass(_OnDevice), a.scales)
+    there, elsewhere = types.SimpleNamespace(device_index=-1), types.SimpleNamespace(device_index=0)
+    calls = [(3, lambda s: B.quantize(fake(4, 256), stream=s)), (2, lambda s: B.norm_in(fake(4, 256), stream=s)),
+             (3, lambda s: B.norm_in(fake(4, 256), scaled=True, stream=s)), (2, lambda s: B.norm_out(fake(4, 256), stream=s)),
+             (3, lambda s: B.norm_out(fake(4, 256), fake(4, 256), next_kind=B.NORM_RMS, stream=s)),
+             (4, lambda s: B.scaled_matmul(a, w, out_dtype=torch.float8_e4m3fn, stream=s))]      # with partial sums
+    for count, call in calls:
+        made.clear()
+        call(there)
+        assert len(made) == count and all(m is there for m in made)
+        with pytest.raises(ValueError):
+            call(elsewhere)
 
 
 def test_the_e4m3_table_of_the_oracle():
