@@ -71,10 +71,13 @@ __device__ __forceinline__ float activated(float g, int act) {
 }
 
 // TPR threads hold a row, thread t columns 8 (i TPR + t) .. + 7, i < NV: 16 lanes hold a block of 128 columns.  WHOLE: d is a
-// multiple of 8, so that no vector ends early (the code for one that does costs every thread registers).
+// multiple of 8, so that no vector ends early (the code for one that does costs every thread registers).  Weights come with the
+// row up to two vectors a thread (4096 x 4096 26.3 us, 30.6 after the row's sum), with four they come when they are needed: the
+// registers allow half the waves otherwise (2048 x 16384 with gate and fp32 residual 102 us, 121; 2048 x 32768 fp32 136, 295).
 template <class T, class S, int TPR, int NV, bool WHOLE>
 __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
   constexpr int WAVES = TPR / 64;
+  constexpr bool EARLY = NV < 4;      // weights loaded with the row
   __shared__ float part[4 * WAVES];
   const int t = threadIdx.x % TPR;
   const int64_t row = (int64_t)blockIdx.x * (TPR == 64 ? 4 : 1) + threadIdx.x / TPR;
@@ -88,8 +91,10 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
     const bool in = col < p.d;
     rb[i] = p.branch && in ? load8((const T*)p.branch + row * p.branch_ld, col, end) : Raw8<T>{};
     rr[i] = p.residual && in ? load8((const S*)p.residual + row * p.residual_ld, col, end) : Raw8<S>{};
-    w[i] = p.weight && in ? load8((const T*)p.weight, col, end) : Raw8<T>{};
-    nw[i] = p.next_weight && in ? load8((const T*)p.next_weight, col, end) : Raw8<T>{};
+    if (EARLY) {
+      w[i] = p.weight && in ? load8((const T*)p.weight, col, end) : Raw8<T>{};
+      nw[i] = p.next_weight && in ? load8((const T*)p.next_weight, col, end) : Raw8<T>{};
+    }
   }
   float v[NV][8];
 #pragma unroll
@@ -102,6 +107,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
     const int col = (i * TPR + t) * 8;
     if (col >= p.d) continue;
     if (p.weight) {
+      if (!EARLY) w[i] = load8((const T*)p.weight, col, end);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] *= w[i].get(e) + p.weight_plus;
     }
@@ -137,6 +143,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
   for (int i = 0; i < NV; ++i) {
     const int col = (i * TPR + t) * 8;
     if (p.next_weight) {
+      if (!EARLY) nw[i] = col < p.d ? load8((const T*)p.next_weight, col, end) : Raw8<T>{};
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] *= nw[i].get(e) + p.weight_plus;
     }
@@ -171,17 +178,22 @@ static void run_norm(const NormP& p, hipStream_t st) {
   else k_norm<T, S, TPR, NV, false><<<wgs, TPR == 64 ? 256 : TPR, 0, st>>>(p);
 }
 
+// As few vectors a thread as a workgroup's size allows: a row's chain (loads, sums over the workgroup, stores) is what a CU has
+// four of at 512 threads.  us in a graph, 1024 / 512 / 256 / 128 threads for the row: 4096 x 4096 in 8 bits with a residual
+// 27.6 / 26.3 / 26.3 / 28.5, one such row 5.0 / 4.6 / 4.9, 8192 x 5120 with gate and fp32 residual - / 109 / 113 / 139.
+static int row_threads(int64_t d) { return d <= 512 ? 64 : d <= 2048 ? 256 : d <= 16384 ? 512 : 1024; }
+
 template <class T, class S>
 static void launch_norm(const NormP& p, hipStream_t st) {
-  // As few vectors a thread as a workgroup's size allows: a row's chain (loads, sums over the workgroup, stores) is what a CU has
-  // four of at 512 threads.  us in a graph, 1024 / 512 / 256 / 128 threads for the row: 4096 x 4096 in 8 bits with a residual
-  // 27.6 / 26.3 / 26.3 / 28.5, one such row 5.0 / 4.6 / 4.9, 8192 x 5120 with gate and fp32 residual - / 109 / 113 / 139.
-  if (p.d <= 512) run_norm<T, S, 64, 1>(p, st);
-  else if (p.d <= 2048) run_norm<T, S, 256, 1>(p, st);
-  else if (p.d <= 4096) run_norm<T, S, 512, 1>(p, st);
+  switch (row_threads(p.d)) {
+    case 64: return run_norm<T, S, 64, 1>(p, st);
+    case 256: return run_norm<T, S, 256, 1>(p, st);
+    case 512: break;
+    default: return run_norm<T, S, 1024, 4>(p, st);
+  }
+  if (p.d <= 4096) run_norm<T, S, 512, 1>(p, st);
   else if (p.d <= 8192) run_norm<T, S, 512, 2>(p, st);
-  else if (p.d <= 16384) run_norm<T, S, 512, 4>(p, st);
-  else run_norm<T, S, 1024, 4>(p, st);
+  else run_norm<T, S, 512, 4>(p, st);
 }
 
 static bool known_norm(int k) { return k == SVDMLP_NORM_NONE || k == SVDMLP_NORM_RMS || k == SVDMLP_NORM_LAYER; }
@@ -217,7 +229,7 @@ extern "C" int svdmlp_norm(const svdmlp_norm_args* a, void* hip_stream) {
   if (a->h && a->h == a->residual && a->h_ld != a->residual_ld) return SVDMLP_INVALID_ARGUMENT;
   if ((a->h && (a->h == a->branch || a->h == a->out)) || (a->out && (a->out == a->residual || a->out == a->branch))) return SVDMLP_INVALID_ARGUMENT;
   if (a->type == SVDMLP_F32 && a->stream_type == SVDMLP_BF16) return SVDMLP_UNSUPPORTED;
-  if (a->d > 32768 || a->rows >= int64_t(1) << 21) return SVDMLP_UNSUPPORTED;   // registers of a workgroup; a grid below 2^31 lanes
+  if (a->d > 32768 || a->rows >= (int64_t(1) << 31) / row_threads(a->d)) return SVDMLP_UNSUPPORTED;   // registers; lanes of a grid
   if (a->rows == 0) return SVDMLP_OK;
   NormP p;
   p.residual = a->residual; p.branch = a->branch; p.weight = a->weight; p.bias = a->bias;

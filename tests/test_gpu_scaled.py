@@ -317,6 +317,7 @@ NORMS = [
     (2, 8193, F32, F32, "layer", "rms", "plain", False, True),
     (3, 20000, BF16, F32, "rms", "rms", "sigmoid", False, False),
     (2, 32768, BF16, BF16, "rms", "rms", None, True, False),
+    (2, 32763, F32, F32, "rms", "layer", "tanh", True, True),
     (700, 384, BF16, BF16, "rms", "rms", "plain", True, False),
     (2100, 1536, BF16, F32, "rms", "rms", "sigmoid", True, False),
     (1030, 4096, BF16, BF16, "rms", "rms", None, False, False),
@@ -403,6 +404,33 @@ def test_no_rows_do_nothing():
     assert B.norm_in(e).shape == (0, 256)
     h, n = B.norm_out(e, e.clone(), scaled=True)
     assert h.shape == (0, 256) and n.codes.shape == (0, 256)
+
+
+def test_more_rows_than_two_million():
+    x = torch.randn((1 << 21) + 5, 16, dtype=BF16, device=dev())
+    got = B.norm_in(x)
+    for rows in (slice(0, 9), slice(-9, None)):
+        assert torch.equal(got[rows], B.norm_in(x[rows]))
+
+
+def test_offsets_beyond_32_bits():
+    """1.1 million rows of 4096: 4.5e9 elements.  The last rows are those of a call of their own; the product's to two bf16
+    roundings and what the matrix instruction drops (2.5e-5 of the result's size in either kernel, 1e-3 allowed)."""
+    M, d = 1_100_000, 4096
+    x = torch.randn(M, d, dtype=BF16, device=dev())
+    last = slice(M - 200, M)
+    got = B.quantize(x)
+    alone = B.quantize(x[last])
+    assert torch.equal(got.codes[last].view(torch.uint8), alone.codes.view(torch.uint8)) and torch.equal(got.scales[:, last], alone.scales)
+    W = B.quantize(torch.randn(24, d, device=dev()), block_rows=128)
+    p, q = B.scaled_matmul(got, W)[last].float(), B.scaled_matmul(alone, W).float()
+    assert ((p - q).abs() <= 2 * 2.0 ** -8 * q.abs() + 1e-3 * q.abs().max()).all()
+    p = B.scaled_matmul(got, W, out_dtype=torch.float8_e4m3fn).scales[:, last].float()
+    q = B.scaled_matmul(alone, W, out_dtype=torch.float8_e4m3fn).scales.float()
+    assert ((p - q).abs() <= 3 * 2.0 ** -8 * q).all()      # either rounded to bf16, and the product's difference in the largest
+    h = torch.empty_like(x)
+    n = B.norm_in(x, h=h)
+    assert torch.equal(n[last], B.norm_in(x[last])) and torch.equal(h[last], x[last])
 
 
 # ---------------------------------------------------------------------------------------------- together

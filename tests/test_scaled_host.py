@@ -85,7 +85,9 @@ def test_quantize_refuses(changed, want):
     (dict(h=0x1000), OK), (dict(h=0x1000, h_ld=300), BAD), (dict(h=0x2000), BAD), (dict(out=0x1000), BAD), (dict(out=0x5000), BAD),
     (dict(type=F32, stream_type=BF16, out_type=F32), UNSUPPORTED), (dict(stream_type=F32), OK), (dict(residual=0), OK), (dict(h=0), OK),
     (dict(d=32769, residual_ld=40000, branch_ld=40000, gate_ld=40000, h_ld=40000, out_ld=40000), UNSUPPORTED),
-    (dict(rows=1 << 21, out_scales_ld=1 << 21), UNSUPPORTED),
+    (dict(rows=1 << 25, out_scales_ld=1 << 25), UNSUPPORTED),
+    (dict(rows=1 << 21, d=16385, residual_ld=40000, branch_ld=40000, gate_ld=40000, h_ld=40000, out_ld=40000, out_scales_ld=1 << 21),
+     UNSUPPORTED),
 ])
 def test_norm_refuses(changed, want):
     assert status("svdmlp_norm", **changed) == want
@@ -99,6 +101,7 @@ def test_norm_refuses(changed, want):
     (dict(out_type=BF16, c=0x5002, c_ld=65), OK), (dict(out_type=BF16, c_ld=63), BAD), (dict(out_type=BF16, c_scales=0), OK),
     (dict(a_ld=1 << 23), UNSUPPORTED), (dict(w_ld=1 << 23), UNSUPPORTED), (dict(M=1 << 24), UNSUPPORTED), (dict(N=(1 << 22) + 1), UNSUPPORTED),
     (dict(K=(1 << 22) + 1), UNSUPPORTED),
+    (dict(M=1 << 23, N=1 << 16, c_ld=1 << 16, a_scales_ld=1 << 23, c_scales_ld=1 << 23), UNSUPPORTED),
 ])
 def test_scaled_matmul_refuses(changed, want):
     assert status("svdmlp_scaled_matmul", **changed) == want
