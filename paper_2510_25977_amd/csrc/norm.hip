@@ -31,8 +31,8 @@ __device__ __forceinline__ float row_sum(float x, float* part) {
   return x;
 }
 
-// v <- its norm, without weight.  Columns beyond d hold zeros and are left out of the second sum of a LAYER norm.
-template <int TPR, int NV>
+// v <- its norm, without weight.  What is not a thread's own holds zeros and is left out of the second sum of a LAYER norm.
+template <int TPR, int NV, RowEnd END>
 __device__ __forceinline__ void normalize(float (&v)[NV][8], int kind, float eps, const NormP& p, int t, float* part) {
   if (kind == SVDMLP_NORM_LAYER) {
     float s = 0.f;
@@ -44,7 +44,7 @@ __device__ __forceinline__ void normalize(float (&v)[NV][8], int kind, float eps
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = (i * TPR + t) * 8 + e < p.d ? v[i][e] - mean : 0.f;
+      for (int e = 0; e < 8; ++e) v[i][e] = Cols<END>((i * TPR + t) * 8, p.d).own(e) ? v[i][e] - mean : 0.f;
     part += TPR / 64;
   }
   float s = 0.f;
@@ -70,11 +70,10 @@ __device__ __forceinline__ float activated(float g, int act) {
   return act == SVDMLP_GATE_SIGMOID ? __builtin_amdgcn_rcpf(1.f + __expf(-g)) : act == SVDMLP_GATE_TANH ? tanh_f32(g) : g;
 }
 
-// TPR threads hold a row, thread t columns 8 (i TPR + t) .. + 7, i < NV: 16 lanes hold a block of 128 columns.  WHOLE: d is a
-// multiple of 8, so that no vector ends early (the code for one that does costs every thread registers).  Weights come with the
+// TPR threads hold a row, thread t columns 8 (i TPR + t) .. + 7, i < NV: 16 lanes hold a block of 128 columns.  Weights come with the
 // row up to two vectors a thread (4096 x 4096 26.3 us, 30.6 after the row's sum), with four they come when they are needed: the
 // registers allow half the waves otherwise (2048 x 16384 with gate and fp32 residual 102 us, 121; 2048 x 32768 fp32 136, 295).
-template <class T, class S, int TPR, int NV, bool WHOLE>
+template <class T, class S, int TPR, int NV, RowEnd END>
 __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
   constexpr int WAVES = TPR / 64;
   constexpr bool EARLY = NV < 4;      // weights loaded with the row
@@ -82,47 +81,47 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
   const int t = threadIdx.x % TPR;
   const int64_t row = (int64_t)blockIdx.x * (TPR == 64 ? 4 : 1) + threadIdx.x / TPR;
   if (row >= p.rows) return;   // whole waves, and whole workgroups where they meet at a barrier
-  const int end = WHOLE ? 0x7fffffff : p.d;     // of a row, as far as a vector that begins inside has to know
   Raw8<T> rb[NV], w[NV], nw[NV];
   Raw8<S> rr[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int col = (i * TPR + t) * 8;
-    const bool in = col < p.d;
-    rb[i] = p.branch && in ? load8((const T*)p.branch + row * p.branch_ld, col, end) : Raw8<T>{};
-    rr[i] = p.residual && in ? load8((const S*)p.residual + row * p.residual_ld, col, end) : Raw8<S>{};
+    const Cols<END> k((i * TPR + t) * 8, p.d);
+    rb[i] = p.branch ? load8((const T*)p.branch + row * p.branch_ld, k) : Raw8<T>{};
+    rr[i] = p.residual ? load8((const S*)p.residual + row * p.residual_ld, k) : Raw8<S>{};
     if (EARLY) {
-      w[i] = p.weight && in ? load8((const T*)p.weight, col, end) : Raw8<T>{};
-      nw[i] = p.next_weight && in ? load8((const T*)p.next_weight, col, end) : Raw8<T>{};
+      w[i] = p.weight ? load8((const T*)p.weight, k) : Raw8<T>{};
+      nw[i] = p.next_weight ? load8((const T*)p.next_weight, k) : Raw8<T>{};
     }
   }
   float v[NV][8];
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i) {
+    const Cols<END> k((i * TPR + t) * 8, p.d);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] = rb[i].get(e);
-  if (p.kind != SVDMLP_NORM_NONE) normalize<TPR, NV>(v, p.kind, p.eps, p, t, part);
+    for (int e = 0; e < 8; ++e) v[i][e] = END == WHOLE || k.own(e) ? rb[i].get(e) : 0.f;
+  }
+  if (p.kind != SVDMLP_NORM_NONE) normalize<TPR, NV, END>(v, p.kind, p.eps, p, t, part);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int col = (i * TPR + t) * 8;
-    if (col >= p.d) continue;
+    const Cols<END> k((i * TPR + t) * 8, p.d);
+    if (!k.any()) continue;
     if (p.weight) {
-      if (!EARLY) w[i] = load8((const T*)p.weight, col, end);
+      if (!EARLY) w[i] = load8((const T*)p.weight, k);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] *= w[i].get(e) + p.weight_plus;
     }
     if (p.bias) {
-      const Raw8<T> b = load8((const T*)p.bias, col, end);
+      const Raw8<T> b = load8((const T*)p.bias, k);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] += b.get(e);
     }
     if (p.branch_scale) {
-      const Raw8<T> s = load8((const T*)p.branch_scale, col, end);
+      const Raw8<T> s = load8((const T*)p.branch_scale, k);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] *= s.get(e);
     }
     if (p.gate) {
-      const Raw8<T> s = load8((const T*)p.gate + row / p.gate_rows * p.gate_ld, col, end);
+      const Raw8<T> s = load8((const T*)p.gate + row / p.gate_rows * p.gate_ld, k);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] *= activated(s.get(e), p.gate_act);
     }
@@ -130,52 +129,50 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] += p.residual_scale * rr[i].get(e);
     }
-    if (!WHOLE) {
+    if (p.h) store8((S*)p.h + row * p.h_ld, k, v[i]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (col + e >= p.d) v[i][e] = 0.f;
-    }
-    if (p.h) store8((S*)p.h + row * p.h_ld, col, end, v[i]);
+    for (int e = 0; e < 8; ++e)
+      if (END != WHOLE && !k.own(e)) v[i][e] = 0.f;
   }
   if (p.next_kind == SVDMLP_NORM_NONE) return;
-  normalize<TPR, NV>(v, p.next_kind, p.next_eps, p, t, part + 2 * WAVES);
+  normalize<TPR, NV, END>(v, p.next_kind, p.next_eps, p, t, part + 2 * WAVES);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int col = (i * TPR + t) * 8;
+    const Cols<END> k((i * TPR + t) * 8, p.d);
     if (p.next_weight) {
-      if (!EARLY) nw[i] = col < p.d ? load8((const T*)p.next_weight, col, end) : Raw8<T>{};
+      if (!EARLY) nw[i] = load8((const T*)p.next_weight, k);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] *= nw[i].get(e) + p.weight_plus;
     }
-    if (p.next_bias && col < p.d) {
-      const Raw8<T> b = load8((const T*)p.next_bias, col, end);
+    if (p.next_bias) {
+      const Raw8<T> b = load8((const T*)p.next_bias, k);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] += b.get(e);
     }
     if (!p.out_f8) {
-      if (col < p.d) store8((T*)p.out + row * p.out_ld, col, end, v[i]);
+      if (k.any()) store8((T*)p.out + row * p.out_ld, k, v[i]);
       continue;
     }
     float amax = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (!WHOLE && col + e >= p.d) v[i][e] = 0.f;
-      amax = fmaxf(amax, fabsf(v[i][e]));
-    }
+    for (int e = 0; e < 8; ++e) amax = END == WHOLE || k.own(e) ? fmaxf(amax, fabsf(v[i][e])) : amax;
     const __bf16 s = scale_of(max16(amax));
-    if (col < p.d) {
-      store_codes8((unsigned char*)p.out + row * p.out_ld, col, end, v[i], 1.f / (float)s);
-      if (t % 16 == 0) p.out_scales[(int64_t)(col / SCALE_BLOCK) * p.out_scales_ld + row] = s;
+    if (k.any()) {
+      store_codes8((unsigned char*)p.out + row * p.out_ld, k, v[i], 1.f / (float)s);
+      if (t % 16 == 0) p.out_scales[(int64_t)((i * TPR + t) / 16) * p.out_scales_ld + row] = s;
     }
   }
 }
 
-template <class T, class S, int TPR, int NV>
+template <class T, class S, int TPR, int NV, RowEnd END>
 static void run_norm(const NormP& p, hipStream_t st) {
   constexpr int per = TPR == 64 ? 4 : 1;
-  const unsigned wgs = (unsigned)((p.rows + per - 1) / per);
-  if (p.d % 8 == 0) k_norm<T, S, TPR, NV, true><<<wgs, TPR == 64 ? 256 : TPR, 0, st>>>(p);
-  else k_norm<T, S, TPR, NV, false><<<wgs, TPR == 64 ? 256 : TPR, 0, st>>>(p);
+  k_norm<T, S, TPR, NV, END><<<(unsigned)((p.rows + per - 1) / per), TPR * per, 0, st>>>(p);
+}
+template <class T, class S, int TPR, int NV>
+static void run_norm(const NormP& p, hipStream_t st) {
+  if (p.d % 8 == 0) run_norm<T, S, TPR, NV, WHOLE>(p, st);
+  else run_norm<T, S, TPR, NV, OVERLAP>(p, st);
 }
 
 // As few vectors a thread as a workgroup's size allows: a row's chain (loads, sums over the workgroup, stores) is what a CU has
@@ -185,6 +182,7 @@ static int row_threads(int64_t d) { return d <= 512 ? 64 : d <= 2048 ? 256 : d <
 
 template <class T, class S>
 static void launch_norm(const NormP& p, hipStream_t st) {
+  if (row_end(p.d) == SHORT) return run_norm<T, S, 64, 1, SHORT>(p, st);
   switch (row_threads(p.d)) {
     case 64: return run_norm<T, S, 64, 1>(p, st);
     case 256: return run_norm<T, S, 256, 1>(p, st);

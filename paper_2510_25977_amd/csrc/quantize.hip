@@ -16,62 +16,57 @@ struct QuantP {
 
 // A group of 16 lanes holds the 128 columns of one row's block, eight a lane.  A workgroup takes 16 rows x QB blocks: the
 // scales of 16 rows lie side by side, and a row's piece is QB * 256 bytes of bf16.
-template <class T, bool GATED, int QB, bool WHOLE>
+template <class T, bool GATED, int QB, RowEnd END>
 __global__ __launch_bounds__(256) void k_quantize(QuantP p) {
   const int g = threadIdx.x / 16, lane = threadIdx.x % 16;
   const int nb = (p.cols + SCALE_BLOCK - 1) / SCALE_BLOCK, strips = (nb + QB - 1) / QB;
   const int64_t row = (int64_t)(blockIdx.x / strips) * 16 + g;
-  const int b0 = (int)(blockIdx.x % strips) * QB, end = WHOLE ? 0x7fffffff : p.cols;
+  const int b0 = (int)(blockIdx.x % strips) * QB;
   if (row >= p.rows) return;
   const T* x = (const T*)p.x + row * p.x_ld;
   const T* u = GATED ? (const T*)p.gated + row * p.gated_ld : nullptr;
   Raw8<T> rx[QB], ru[QB];
 #pragma unroll
   for (int i = 0; i < QB; ++i) {
-    const int col = (b0 + i) * SCALE_BLOCK + lane * 8;
-    if (col < p.cols) {
-      rx[i] = load8(x, col, end);
-      if (GATED) ru[i] = load8(u, col, end);
-    } else {
-      rx[i] = Raw8<T>{};
-      if (GATED) ru[i] = Raw8<T>{};
-    }
+    const Cols<END> k((b0 + i) * SCALE_BLOCK + lane * 8, p.cols);
+    rx[i] = load8(x, k);
+    if (GATED) ru[i] = load8(u, k);
   }
 #pragma unroll
   for (int i = 0; i < QB; ++i) {
-    const int col = (b0 + i) * SCALE_BLOCK + lane * 8;
+    const Cols<END> k((b0 + i) * SCALE_BLOCK + lane * 8, p.cols);
     float v[8], amax = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       v[e] = rx[i].get(e);
       if (GATED) v[e] *= __builtin_amdgcn_rcpf(1.f + __expf(-v[e])) * ru[i].get(e);
-      amax = fmaxf(amax, fabsf(v[e]));
+      amax = END == WHOLE || k.own(e) ? fmaxf(amax, fabsf(v[e])) : amax;
     }
     const __bf16 s = scale_of(max16(amax));
-    if (col < p.cols) store_codes8(p.codes + row * p.codes_ld, col, end, v, 1.f / (float)s);
+    if (k.any()) store_codes8(p.codes + row * p.codes_ld, k, v, 1.f / (float)s);
     if (lane == 0 && b0 + i < nb) ((__bf16*)p.scales)[(int64_t)(b0 + i) * p.scales_ld + row] = s;
   }
 }
 
 // Weights, once: a workgroup per 128 x 128 block.
-template <class T>
+template <class T, RowEnd END>
 __global__ __launch_bounds__(256) void k_quantize_block(QuantP p) {
   __shared__ float part[4];
   const int g = threadIdx.x / 16, lane = threadIdx.x % 16;
   const int kb = (p.cols + SCALE_BLOCK - 1) / SCALE_BLOCK;
   const int64_t r0 = (int64_t)(blockIdx.x / kb) * SCALE_BLOCK;
-  const int col = (int)(blockIdx.x % kb) * SCALE_BLOCK + lane * 8;
+  const Cols<END> k((int)(blockIdx.x % kb) * SCALE_BLOCK + lane * 8, p.cols);
   Raw8<T> r[8];
   float amax = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = r0 + g + 16 * i;
-    r[i] = row < p.rows && col < p.cols ? load8((const T*)p.x + row * p.x_ld, col, p.cols) : Raw8<T>{};
+    r[i] = row < p.rows ? load8((const T*)p.x + row * p.x_ld, k) : Raw8<T>{};
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(r[i].get(e)));
+    for (int e = 0; e < 8; ++e) amax = END == WHOLE || k.own(e) ? fmaxf(amax, fabsf(r[i].get(e))) : amax;
   amax = max16(amax);
   amax = fmaxf(amax, __shfl_xor(amax, 16));
   amax = fmaxf(amax, __shfl_xor(amax, 32));
@@ -84,29 +79,32 @@ __global__ __launch_bounds__(256) void k_quantize_block(QuantP p) {
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = r[i].get(e);
-    if (row < p.rows && col < p.cols) store_codes8(p.codes + row * p.codes_ld, col, p.cols, v, 1.f / s);
+    if (row < p.rows && k.any()) store_codes8(p.codes + row * p.codes_ld, k, v, 1.f / s);
   }
   if (threadIdx.x == 0) ((float*)p.scales)[blockIdx.x] = s;
 }
 
-// Four blocks a group where no vector ends early, one where each is stored with the code for that: 1 / 2 / 4 blocks take, in a
-// graph, 66.8 / 63.6 / 59.0 us at 4096 x 14336 gated, 6.0 / 5.6 / 5.2 us at 16 x 14336, 19.9 / 20.7 / 21.5 us at 1777 x 7301.
-template <class T, bool GATED>
+// 1 / 2 / 4 blocks a group take, in a graph, 66.8 / 63.6 / 59.0 us at 4096 x 14336 gated, 6.0 / 5.6 / 5.2 us at 16 x 14336; with
+// four, 1777 x 7301 gated takes 15.1 us (4.3 TB/s), 1777 x 7304 14.4.  Rows of less than eight columns have one block.
+template <class T, bool GATED, int QB, RowEnd END>
 static void run_quantize(const QuantP& p, hipStream_t st) {
   const int64_t strips = (p.rows + 15) / 16, nb = scale_blocks(p.cols);
-  if (p.cols % 8 == 0) k_quantize<T, GATED, 4, true><<<(unsigned)(strips * ((nb + 3) / 4)), 256, 0, st>>>(p);
-  else k_quantize<T, GATED, 1, false><<<(unsigned)(strips * nb), 256, 0, st>>>(p);
+  k_quantize<T, GATED, QB, END><<<(unsigned)(strips * ((nb + QB - 1) / QB)), 256, 0, st>>>(p);
 }
-
+template <class T, RowEnd END>
+static void launch_quantize(const QuantP& p, bool weights, hipStream_t st) {
+  constexpr int QB = END == SHORT ? 1 : 4;
+  if (weights) k_quantize_block<T, END><<<(unsigned)(scale_blocks(p.rows) * scale_blocks(p.cols)), 256, 0, st>>>(p);
+  else if (p.gated) run_quantize<T, true, QB, END>(p, st);
+  else run_quantize<T, false, QB, END>(p, st);
+}
 template <class T>
 static void launch_quantize(const QuantP& p, bool weights, hipStream_t st) {
-  const int64_t nb = scale_blocks(p.cols);
-  if (weights) {
-    k_quantize_block<T><<<(unsigned)(scale_blocks(p.rows) * nb), 256, 0, st>>>(p);
-    return;
+  switch (row_end(p.cols)) {
+    case WHOLE: return launch_quantize<T, WHOLE>(p, weights, st);
+    case OVERLAP: return launch_quantize<T, OVERLAP>(p, weights, st);
+    case SHORT: return launch_quantize<T, SHORT>(p, weights, st);
   }
-  if (p.gated) run_quantize<T, true>(p, st);
-  else run_quantize<T, false>(p, st);
 }
 
 }  // namespace svdmlp

@@ -589,31 +589,31 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 }
 
 // Adds the ranges' partial sums in their order and rounds: 16 lanes hold 128 columns of a row, a workgroup 16 rows of them.
-template <int JOIN>      // ranges whose loads are issued together
+template <int JOIN, RowEnd END>      // JOIN: ranges whose loads are issued together
 __global__ __launch_bounds__(256) void k_mm_join(MmP p) {
   const int lane = threadIdx.x % 16, nb = (p.N + SCALE_BLOCK - 1) / SCALE_BLOCK;
-  const int m = (int)(blockIdx.x / nb) * 16 + threadIdx.x / 16, b = (int)(blockIdx.x % nb), n = b * SCALE_BLOCK + 8 * lane;
+  const int m = (int)(blockIdx.x / nb) * 16 + threadIdx.x / 16, b = (int)(blockIdx.x % nb);
   if (m >= p.M) return;
+  const Cols<END> k(b * SCALE_BLOCK + 8 * lane, p.N);
   float v[8] = {};
-  if (n < p.N)
-    for (int z = 0; z < p.ranges; z += JOIN) {
-      Raw8<float> x[JOIN];
+  for (int z = 0; z < p.ranges; z += JOIN) {
+    Raw8<float> x[JOIN];
 #pragma unroll
-      for (int i = 0; i < JOIN; ++i) x[i] = z + i < p.ranges ? load8(p.part + ((int64_t)(z + i) * p.M + m) * p.N, n, p.N) : Raw8<float>{};
+    for (int i = 0; i < JOIN; ++i) x[i] = z + i < p.ranges ? load8(p.part + ((int64_t)(z + i) * p.M + m) * p.N, k) : Raw8<float>{};
 #pragma unroll
-      for (int i = 0; i < JOIN; ++i)
+    for (int i = 0; i < JOIN; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += x[i].get(e);
-    }
+      for (int e = 0; e < 8; ++e) v[e] += x[i].get(e);
+  }
   if (p.out_type == SVDMLP_F8) {
     float amax = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[e]));
+    for (int e = 0; e < 8; ++e) amax = k.own(e) ? fmaxf(amax, fabsf(v[e])) : amax;
     const __bf16 s = scale_of(max16(amax));
-    if (n < p.N) store_codes8((unsigned char*)p.c + m * p.c_ld, n, p.N, v, 1.f / (float)s);
+    if (k.any()) store_codes8((unsigned char*)p.c + m * p.c_ld, k, v, 1.f / (float)s);
     if (lane == 0) p.c_scales[b * p.c_scales_ld + m] = s;
-  } else if (n < p.N) {
-    store8((__bf16*)p.c + m * p.c_ld, n, p.N, v);
+  } else if (k.any()) {
+    store8((__bf16*)p.c + m * p.c_ld, k, v);
   }
 }
 
@@ -697,12 +697,20 @@ static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, MmPlan* best) 
 
 static size_t part_bytes(const MmPlan& q, int64_t M, int64_t N) { return q.join ? (size_t)q.ranges * M * N * 4 : 0; }
 
+template <RowEnd END>
 static void launch_join(const MmP& p, hipStream_t st) {
   const unsigned wgs = (unsigned)((p.M + 15) / 16 * scale_blocks(p.N));
-  if (p.ranges == 1) k_mm_join<1><<<wgs, 256, 0, st>>>(p);
-  else if (p.ranges <= 4) k_mm_join<4><<<wgs, 256, 0, st>>>(p);
-  else if (p.ranges <= 8) k_mm_join<8><<<wgs, 256, 0, st>>>(p);
-  else k_mm_join<16><<<wgs, 256, 0, st>>>(p);
+  if (p.ranges == 1) k_mm_join<1, END><<<wgs, 256, 0, st>>>(p);
+  else if (p.ranges <= 4) k_mm_join<4, END><<<wgs, 256, 0, st>>>(p);
+  else if (p.ranges <= 8) k_mm_join<8, END><<<wgs, 256, 0, st>>>(p);
+  else k_mm_join<16, END><<<wgs, 256, 0, st>>>(p);
+}
+static void launch_join(const MmP& p, hipStream_t st) {
+  switch (row_end(p.N)) {
+    case WHOLE: return launch_join<WHOLE>(p, st);
+    case OVERLAP: return launch_join<OVERLAP>(p, st);
+    case SHORT: return k_mm_join<4, SHORT><<<(unsigned)((p.M + 15) / 16), 256, 0, st>>>(p);
+  }
 }
 
 static void launch_mm(MmP& p, const MmPlan& q, hipStream_t st) {

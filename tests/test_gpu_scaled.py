@@ -122,7 +122,8 @@ MATMULS = [
     (1, 1, 1), (1, 16, 128), (2, 7, 15), (3, 130, 16), (5, 64, 17), (15, 129, 100), (16, 512, 127), (17, 100, 128),
     (16, 300, 129), (31, 128, 255), (32, 257, 256), (33, 96, 257), (47, 200, 640), (64, 512, 1000), (1, 1000, 2304),
     (63, 33, 3000), (65, 384, 513), (100, 127, 2000), (128, 256, 384), (129, 255, 383), (200, 520, 1152), (256, 256, 512),
-    (257, 640, 300), (300, 1000, 270), (513, 515, 517), (1000, 700, 1100), (40, 3000, 400), (2, 16, 9000), (130, 40, 9001),
+    (257, 640, 300), (300, 1000, 270), (513, 515, 517), (1000, 700, 1100), (40, 3000, 400), (2, 16, 9000), (130, 40, 9001), (7, 9, 3000),
+    (20, 15, 5000), (1, 131, 4000), (64, 259, 4000),
     # what else the product's kernels and their cuts of the contraction are chosen for (a host test sees to it that all are here)
     (3, 6000, 300), (700, 500, 1300), (520, 300, 2500), (700, 4100, 400), (90, 1100, 4000), (2741, 2252, 135), (1301, 4999, 300),
     (1290, 5000, 513), (300, 2600, 6000), (2100, 5000, 257), (2111, 4983, 600), (1500, 600, 9000), (3, 66, 555), (284, 1738, 1842),
@@ -193,7 +194,8 @@ def test_zero_activations_give_zeros_whatever_their_scale():
 
 
 # ---------------------------------------------------------------------------------------------- quantiser
-QUANTIZE = [(1, 1), (1, 128), (2, 7), (3, 129), (16, 256), (17, 1000), (33, 127), (100, 2687), (130, 385), (257, 136)]
+QUANTIZE = [(1, 1), (1, 128), (2, 7), (3, 129), (16, 256), (17, 1000), (33, 127), (100, 2687), (130, 385), (257, 136),
+            (20, 9), (5, 15), (35, 263), (18, 644)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
@@ -303,6 +305,9 @@ NORMS = [
     # rows, row length, types, norm after, norm before the next, gate, scale per channel, bias
     (1, 1, BF16, BF16, "rms", "rms", None, False, False),
     (1, 4096, BF16, BF16, "none", "rms", None, False, False),
+    (5, 7, BF16, F32, "layer", "rms", "tanh", True, True),
+    (6, 9, BF16, BF16, "rms", "layer", None, True, True),
+    (70, 263, F32, F32, "layer", "layer", "sigmoid", True, True),
     (3, 127, BF16, F32, "rms", "rms", "plain", True, True),
     (5, 129, F32, F32, "layer", "layer", "sigmoid", False, True),
     (7, 511, BF16, BF16, "none", "layer", "tanh", True, False),
@@ -359,7 +364,7 @@ def test_norm_out(M, d, dtype, stream, post, nxt, act, branch_scale, bias, scale
         assert torch.equal(buf, before)
 
 
-@pytest.mark.parametrize("M,d", [(1, 4096), (40, 1000), (300, 5120)])
+@pytest.mark.parametrize("M,d", [(1, 4096), (40, 1000), (300, 5120), (400, 515), (300, 4099), (40, 2687), (200, 8190)])
 def test_norm_in_and_its_in_place_residual(M, d):
     """norm_in without and with what is added; h in the place of x gives the same bits as h elsewhere; norm_out without the
     next norm, the residual's buffer as its h."""
