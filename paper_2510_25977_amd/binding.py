@@ -8,7 +8,6 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import struct
 from pathlib import Path
 from typing import NamedTuple, Optional
 
@@ -16,6 +15,7 @@ import torch
 
 HERE = Path(__file__).resolve().parent
 LIB_PATH = HERE / "libsvdmlp.so"      # the in-tree build, nothing else
+TENSORS_PATH = HERE / "_tensors.so"
 
 SVDMLP_BF16, SVDMLP_F32 = 0, 1
 SVDMLP_GATED, SVDMLP_LINEAR = 0, 1
@@ -49,13 +49,6 @@ class svdmlp_desc(ctypes.Structure):
         ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
         ("flags", ctypes.c_uint32),
     ]
-
-
-# The operators' argument structures of the header, field for field, as struct formats: a call packs its arguments into bytes
-# (1 us for the longest; filling a ctypes.Structure takes three times that, and the smallest calls are bound by it).
-QUANTIZE_ARGS = struct.Struct("=qqiiQQqqQQqq")
-NORM_ARGS = struct.Struct("=qqiiiiiiqffffQQqqQQQQqQQQqQqQq")
-SCALED_MATMUL_ARGS = struct.Struct("=qqqiiQQqqQQqQQqqQQ")
 
 
 class SvdMlpError(RuntimeError):
@@ -368,7 +361,9 @@ class Scaled(NamedTuple):
 def empty_scaled(rows: int, cols: int, device, block_rows: int = 1) -> Scaled:
     """An uninitialised 8-bit tensor, rows of codes padded to 16 bytes."""
     blocks = -(-cols // SCALE_BLOCK)
-    codes = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+    codes = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)
+    if cols % 16:
+        codes = codes[:, :cols]
     if block_rows == 1:
         return Scaled(codes, torch.empty((blocks, rows), dtype=torch.bfloat16, device=device))
     return Scaled(codes, torch.empty((-(-rows // SCALE_BLOCK), blocks), dtype=torch.float32, device=device))
@@ -377,47 +372,17 @@ def empty_scaled(rows: int, cols: int, device, block_rows: int = 1) -> Scaled:
 _F8, _BF16 = torch.float8_e4m3fn, torch.bfloat16
 
 
-# The smallest calls are bound by what follows, so it asks a tensor for little: 0.4 us each.
-def _refuse(t, what: str, shape, dtype, device: int):
-    raise ValueError(f"{what} must be a {tuple(shape)} {dtype} tensor on cuda:{device} whose rows lie in one piece, "
-                     f"got {tuple(t.shape)} {t.dtype} on {t.device} with strides {t.stride()}")
+_checks = None
 
 
-def _rows(t: torch.Tensor, what: str, shape, dtype, device: int, multiple: int = 1):
-    """(address, row stride) of a matrix on `device`: rows of consecutive elements, any stride between them."""
-    stride = t.stride()
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or (stride[1] != 1 and shape[1] != 1):
-        _refuse(t, what, shape, dtype, device)
-    # the stride of a single row says nothing
-    return t.data_ptr(), stride[0] if shape[0] > 1 else (shape[1] + multiple - 1) // multiple * multiple
-
-
-def _vector(t: Optional[torch.Tensor], what: str, n: int, dtype, device: int) -> int:
-    if t is None:
-        return 0
-    if t.shape != (n,) or t.dtype is not dtype or t.get_device() != device or (n > 1 and t.stride()[0] != 1):
-        _refuse(t, what, (n,), dtype, device)
-    return t.data_ptr()
-
-
-def _codes(t, what: str, shape, device: int):
-    """(codes, codes stride, scales, scales stride) of activations"""
-    codes, scales = t
-    ptr, ld = _rows(codes, what, shape, _F8, device, 16)
-    rows = shape[0]
-    sptr, sld = _rows(scales, "the scales of " + what, ((shape[1] + SCALE_BLOCK - 1) // SCALE_BLOCK, rows), _BF16, device)
-    return ptr, ld, sptr, sld
-
-
-def _weight_codes(t, what: str, shape, device: int):
-    """(codes, codes stride, scales) of weights"""
-    codes, scales = t
-    ptr, ld = _rows(codes, what, shape, _F8, device, 16)
-    want = (-(-shape[0] // SCALE_BLOCK), -(-shape[1] // SCALE_BLOCK))
-    sptr, sld = _rows(scales, "the scales of " + what, want, torch.float32, device)
-    if sld != want[1]:
-        _refuse(scales, "the (contiguous) scales of " + what, want, torch.float32, device)
-    return ptr, ld, sptr
+def _tensors():
+    """The extension module that checks tensors and packs arguments (raises if it has not been built)."""
+    global _checks
+    if _checks is None:
+        if not TENSORS_PATH.exists():
+            raise FileNotFoundError(f"{TENSORS_PATH} not found: build it with `python -m paper_2510_25977_amd.build`")
+        from . import _tensors as _checks
+    return _checks
 
 
 def _device_of(t: torch.Tensor, what: str) -> int:
@@ -439,15 +404,15 @@ def _on(stream: torch.cuda.Stream, op, t, *args, **kw):
         return op(t, *args, **kw)
 
 
-def _run(name: str, rows: int, args: bytes, device: int) -> None:
-    if rows == 0:            # a tensor of no rows has no address
+def _run(name: str, args: Optional[bytes], device: int) -> None:
+    if args is None:         # no rows
         return
-    s = _current_raw_stream(device)
-    if device != _current_device():          # kernels are launched on the current device
+    op = getattr(lib(), name)
+    if device == _current_device():
+        st = op(args, _current_raw_stream(device))
+    else:                    # kernels are launched on the current device
         with torch.cuda.device(device):
-            st = getattr(lib(), name)(args, s)
-    else:
-        st = getattr(lib(), name)(args, s)
+            st = op(args, _current_raw_stream(device))
     if st != SVDMLP_OK:
         raise SvdMlpError(st, name)
 
@@ -458,59 +423,37 @@ def quantize(x: torch.Tensor, gate_with: Optional[torch.Tensor] = None, *, block
     128 x 128).  x: [R, C] bfloat16 or float32."""
     if stream is not None:
         return _on(stream, quantize, x, gate_with, block_rows=block_rows, out=out)
-    dev, shape, dtype = _device_of(x, "x"), x.shape, x.dtype
-    if dtype not in _TORCH_DTYPE:
-        raise ValueError("x must be bfloat16 or float32")
-    R, C = shape
-    xp, xld = _rows(x, "x", shape, dtype, dev)
-    gp, gld = (0, 0) if gate_with is None else _rows(gate_with, "gate_with", shape, dtype, dev)
+    dev = _device_of(x, "x")
     if out is None:
-        out = empty_scaled(R, C, x.device, block_rows)
-    if block_rows == 1:
-        cp, cld, sp, sld = _codes(out, "out", shape, dev)
-    else:
-        (cp, cld, sp), sld = _weight_codes(out, "out", shape, dev), 0
-    _run("svdmlp_quantize", R, QUANTIZE_ARGS.pack(R, C, _TORCH_DTYPE[dtype], block_rows, xp, gp, xld, gld, cp, sp, cld, sld), dev)
-    return Scaled(*out)
+        out = empty_scaled(*x.shape, x.device, block_rows)
+    codes, scales = out
+    _run("svdmlp_quantize", _tensors().quantize_args(dev, x, gate_with, block_rows, codes, scales), dev)
+    return out if type(out) is Scaled else Scaled(codes, scales)
 
 
 def _norm(x, branch, residual, weight, bias, kind, eps, weight_plus, residual_scale, branch_scale, gate, gate_rows, gate_act,
           next_weight, next_bias, next_kind, next_eps, h, out, scaled, want_h):
     """x: the residual, or the branch where there is none: of the residual stream's type"""
-    dev, shape, stream_dtype = _device_of(x, "x"), x.shape, x.dtype
-    M, d = shape
-    # the type of everything but the residual stream
-    of = branch if branch is not None else weight if weight is not None else next_weight
-    dtype = of.dtype if of is not None else bias.dtype if bias is not None else next_bias.dtype if next_bias is not None else stream_dtype
-    if dtype not in _TORCH_DTYPE or stream_dtype not in _TORCH_DTYPE:
-        raise ValueError("inputs must be bfloat16 or float32")
-    rp, rld = (0, 0) if residual is None else _rows(residual, "residual", shape, stream_dtype, dev)
-    bp, bld = (0, 0) if branch is None else _rows(branch, "branch", shape, dtype, dev)
-    gp = gld = 0
-    if gate is not None:
-        if gate_rows < 1:
-            raise ValueError("gate_rows must be at least 1")
-        gp, gld = _rows(gate, "gate", (-(-M // gate_rows), d), dtype, dev)
+    dev = _device_of(x, "x")
     if h is None and want_h:
-        h = torch.empty((M, d), dtype=stream_dtype, device=x.device)
-    hp, hld = (0, 0) if h is None else _rows(h, "h", shape, stream_dtype, dev)
-    op = old = sp = sld = 0
-    out_type = _TORCH_DTYPE[dtype]
-    if next_kind != NORM_NONE:
-        if out is None:
-            out = empty_scaled(M, d, x.device) if scaled else torch.empty((M, d), dtype=dtype, device=x.device)
-        if isinstance(out, tuple):
-            out_type = SVDMLP_F8
-            op, old, sp, sld = _codes(out, "out", shape, dev)
-            out = Scaled(*out)
+        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if next_kind == NORM_NONE:
+        if out is not None or scaled:
+            raise ValueError("out is what the next norm makes, and there is none")
+    elif out is None:
+        if scaled:
+            out = empty_scaled(*x.shape, x.device)
         else:
-            op, old = _rows(out, "out", shape, dtype, dev)
-    args = NORM_ARGS.pack(
-        M, d, _TORCH_DTYPE[dtype], _TORCH_DTYPE[stream_dtype], out_type, kind, next_kind, gate_act, gate_rows, eps, next_eps,
-        weight_plus, residual_scale, rp, bp, rld, bld, _vector(weight, "weight", d, dtype, dev), _vector(bias, "bias", d, dtype, dev),
-        _vector(branch_scale, "branch_scale", d, dtype, dev), gp, gld, _vector(next_weight, "next_weight", d, dtype, dev),
-        _vector(next_bias, "next_bias", d, dtype, dev), hp, hld, op, old, sp, sld)
-    _run("svdmlp_norm", M, args, dev)
+            of = next((t for t in (branch, weight, next_weight, bias, next_bias) if t is not None), x)
+            out = torch.empty(x.shape, dtype=of.dtype, device=x.device)
+    if isinstance(out, tuple):
+        out = out if type(out) is Scaled else Scaled(*out)
+        codes, scales = out
+    else:
+        codes, scales = out, None
+    args = _tensors().norm_args(dev, branch, residual, weight, bias, kind, eps, weight_plus, residual_scale, branch_scale, gate,
+                                gate_rows, gate_act, next_weight, next_bias, next_kind, next_eps, h, codes, scales)
+    _run("svdmlp_norm", args, dev)
     return h, out
 
 
@@ -561,31 +504,25 @@ def scaled_matmul(a, w, *, out=None, out_dtype: torch.dtype = torch.bfloat16, st
     torch.float8_e4m3fn (or a ``Scaled`` as ``out``) makes it the next product's activations."""
     if stream is not None:
         return _on(stream, scaled_matmul, tuple(a), w, out=out, out_dtype=out_dtype)
-    codes = a[0]
-    dev, shape = _device_of(codes, "a"), codes.shape
-    M, K = shape
-    if w[0].dim() != 2:
+    codes, scales = a
+    w_codes, w_scales = w
+    dev = _device_of(codes, "a")
+    M, K = codes.shape
+    if w_codes.dim() != 2:
         raise ValueError(f"w must be [N, {K}]")
-    N = w[0].shape[0]
-    ap, ald, asp, asld = _codes(a, "a", shape, dev)
-    wp, wld, wsp = _weight_codes(w, "w", (N, K), dev)
+    N = w_codes.shape[0]
     if out is None:
         if out_dtype is not _BF16 and out_dtype is not _F8:
             raise ValueError("out_dtype must be bfloat16 or float8_e4m3fn")
         out = empty_scaled(M, N, codes.device) if out_dtype is _F8 else torch.empty((M, N), dtype=_BF16, device=codes.device)
-    out_type, csp, csld = SVDMLP_BF16, 0, 0
     if isinstance(out, tuple):
-        out_type = SVDMLP_F8
-        cp, cld, csp, csld = _codes(out, "out", (M, N), dev)
-        out = Scaled(*out)
+        out = out if type(out) is Scaled else Scaled(*out)
+        c, c_scales = out
     else:
-        cp, cld = _rows(out, "out", (M, N), _BF16, dev)
-    need, ws = svdmlp_scaled_matmul_workspace_bytes(M, N, K, out_type), 0
-    if need:
-        space = torch.empty(need, dtype=torch.uint8, device=codes.device)
-        ws = space.data_ptr()
-    _run("svdmlp_scaled_matmul", M, SCALED_MATMUL_ARGS.pack(M, N, K, out_type, 0, ap, asp, ald, asld, wp, wsp, wld, cp, csp, cld, csld,
-                                                            ws, need), dev)
+        c, c_scales = out, None
+    need = svdmlp_scaled_matmul_workspace_bytes(M, N, K, SVDMLP_BF16 if c_scales is None else SVDMLP_F8)
+    space = torch.empty(need, dtype=torch.uint8, device=codes.device) if need else None
+    _run("svdmlp_scaled_matmul", _tensors().scaled_matmul_args(dev, M, N, K, codes, scales, w_codes, w_scales, c, c_scales, space), dev)
     return out
 
 

@@ -1,9 +1,9 @@
-"""Build the svdmlp shared library (hipcc, gfx950 only) in-tree.
+"""Build the svdmlp shared library (hipcc, gfx950 only) and the binding's tensor checks (C++) in-tree.
 
     python -m paper_2510_25977_amd.build [--force]
 
-The library is built next to this file as ``libsvdmlp.so`` so that it travels with the source
-tree; tests, ``bench.py`` and ``__graft_entry__.smoke()`` load that file and never compile.
+Both are built next to this file, as ``libsvdmlp.so`` and ``_tensors.so``, so that they travel with the source
+tree; tests, ``bench.py`` and ``__graft_entry__.smoke()`` load these files and never compile.
 """
 from __future__ import annotations
 
@@ -17,6 +17,7 @@ from pathlib import Path
 HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libsvdmlp.so"
+TENSORS = HERE / "_tensors.so"
 OBJDIR = HERE / "_build"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -78,12 +79,27 @@ def check_sgpr_hazards(asm: str) -> list:
     return found
 
 
+def build_tensors() -> None:
+    """Compile the extension module of the binding against the installed torch."""
+    import sysconfig
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    includes = [f"-I{p}" for p in [*include_paths(), sysconfig.get_path("include")]]
+    libs = Path(torch.__file__).resolve().parent / "lib"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *includes, str(CSRC / "tensors.cpp"), "-o", str(TENSORS),
+           f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("the C++ compiler failed on tensors.cpp:\n" + (res.stdout + res.stderr)[-4000:])
+
+
 def build(force: bool = True, verbose: bool = False) -> Path:
-    """Compile every HIP source and link ``libsvdmlp.so``.  Always recompiles unless force=False and
-    the library is newer than every source."""
+    """Compile every HIP source and link ``libsvdmlp.so``, and compile ``_tensors.so``.  Always recompiles unless force=False
+    and both are newer than every source."""
     srcs = sources()
-    deps = srcs + sorted(CSRC.glob("*.h")) + [HERE.parent / "include" / "svdmlp.h"]
-    if not force and LIB.exists() and all(LIB.stat().st_mtime >= s.stat().st_mtime for s in deps):
+    deps = srcs + sorted(CSRC.glob("*.h")) + [CSRC / "tensors.cpp", HERE.parent / "include" / "svdmlp.h"]
+    if not force and all(lib.exists() and all(lib.stat().st_mtime >= s.stat().st_mtime for s in deps) for lib in (LIB, TENSORS)):
         return LIB
     OBJDIR.mkdir(exist_ok=True)
 
@@ -109,10 +125,12 @@ def build(force: bool = True, verbose: bool = False) -> Path:
 
     # sources with hand-written memory instructions that take an SGPR base: their generated assembly is checked
     asm_srcs = [s for s in srcs if re.search(r'asm volatile\("[^;]*global_(load|store)', s.read_text())]
-    with ThreadPoolExecutor(max_workers=min(8, len(srcs) + len(asm_srcs))) as ex:
+    with ThreadPoolExecutor(max_workers=min(8, len(srcs) + len(asm_srcs) + 1)) as ex:
+        tensors = ex.submit(build_tensors)
         hz = [ex.submit(hazards_of, s) for s in asm_srcs]
         objs = list(ex.map(compile_one, srcs))
         hazards = [f for h in hz for f in h.result()]
+        tensors.result()
     if hazards:
         raise RuntimeError("SGPR-to-memory-address hazard inside inline asm (see check_sgpr_hazards):\n" + "\n".join(hazards))
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", str(LIB), *map(str, objs)]

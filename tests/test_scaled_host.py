@@ -1,6 +1,7 @@
 """Host-only checks of the 8-bit operators: what they refuse, before anything touches a device, and the 64-bit oracle."""
 import ctypes
 import re
+import struct
 import types
 
 import numpy as np
@@ -23,8 +24,9 @@ NORM = dict(rows=0, d=256, type=BF16, stream_type=BF16, out_type=F8, kind=B.NORM
             next_bias=0x3000, h=0x5000, h_ld=256, out=0x6000, out_ld=256, out_scales=0x7000, out_scales_ld=64)
 MATMUL = dict(M=0, N=64, K=256, out_type=F8, reserved=0, a=0x1000, a_scales=0x2000, a_ld=256, a_scales_ld=64, w=0x3000, w_scales=0x4000,
               w_ld=256, c=0x5000, c_scales=0x6000, c_ld=64, c_scales_ld=64, workspace=0x7000, workspace_bytes=1 << 30)
-CALLS = {"svdmlp_quantize": (QUANTIZE, B.QUANTIZE_ARGS), "svdmlp_norm": (NORM, B.NORM_ARGS),
-         "svdmlp_scaled_matmul": (MATMUL, B.SCALED_MATMUL_ARGS)}
+CALLS = {"svdmlp_quantize": (QUANTIZE, struct.Struct("=qqiiQQqqQQqq")),
+         "svdmlp_norm": (NORM, struct.Struct("=qqiiiiiiqffffQQqqQQQQqQQQqQqQq")),
+         "svdmlp_scaled_matmul": (MATMUL, struct.Struct("=qqqiiQQqqQQqQQqqQQ"))}
 
 
 def status(name, **changed):
@@ -34,7 +36,7 @@ def status(name, **changed):
 
 
 def test_packed_arguments_are_the_headers_structures():
-    """The struct formats of the binding field for field against the header: order, kind and size."""
+    """The struct formats of these tests field for field against the header: order, kind and size."""
     text = re.sub(r"/\*.*?\*/", "", (ROOT / "include" / "svdmlp.h").read_text(), flags=re.S)
     for name, (fields, layout) in CALLS.items():
         body = re.search(r"typedef struct \{([^}]*)\}\s*" + name + "_args;", text).group(1)
@@ -172,6 +174,9 @@ def test_the_binding_checks_tensors(monkeypatch):
                  lambda: B.norm_in(x, fake(255)), lambda: B.norm_in(x, fake(256, dtype=torch.float16)),
                  lambda: B.norm_in(x, add=fake(5, 256)), lambda: B.norm_in(x, h=fake(4, 256, dtype=torch.float32)),
                  lambda: B.norm_in(x, out=fake(4, 256, dtype=torch.float32)), lambda: B.norm_out(x, x, gate=fake(3, 256)),
+                 lambda: B.norm_out(x, x, out=x.clone(), next_kind=B.NORM_NONE), lambda: B.norm_in(x, kind=B.NORM_NONE, scaled=True),
+                 lambda: B.quantize(x, out=(good.codes, None)), lambda: B.norm_in(x, [1.0], out=x.clone()),
+                 lambda: B.quantize(x, block_rows=1 << 40, out=weights), lambda: B.norm_in(x, kind=1 << 35),
                  lambda: B.norm_out(x, x, gate=x, gate_rows=0), lambda: B.norm_out(x, x, gate=x, gate_rows=2),
                  lambda: B.scaled_matmul(pair, B.empty_scaled(64, 128, "cpu", 128)),
                  lambda: B.scaled_matmul(pair, (weights.codes, weights.scales.t())),
@@ -185,6 +190,73 @@ def test_the_binding_checks_tensors(monkeypatch):
         B.SvdMlpF8(Ug=fake(256, 64), Vg=fake(64, 512))                                        # four factors missing
     with pytest.raises(ValueError):
         B.SvdMlpF8(Ug=fake(256, 64), Vg=fake(65, 512), kind=B.SVDMLP_LINEAR)
+
+
+def fields_of(monkeypatch, call):
+    """The argument structure that a call of the binding hands over, by field."""
+    got = []
+    monkeypatch.setattr(B, "_run", lambda name, args, device: got.append((name, args, device)))
+    call()
+    (name, args, device), = got
+    names, layout = CALLS[name]
+    assert device == -1
+    return None if args is None else dict(zip(names, layout.unpack(args)))
+
+
+def test_what_the_binding_hands_over(monkeypatch):
+    """Every field of every structure, from tensors whose addresses and strides all differ."""
+    def strided(rows, cols, dtype, pad):
+        return torch.zeros(rows, cols + pad).to(dtype)[:, :cols].as_subclass(_OnDevice)
+
+    def f8(rows, cols, pad, spad):
+        return strided(rows, cols, torch.float8_e4m3fn, pad), strided(-(-cols // 128), rows, torch.bfloat16, spad)
+
+    bf, f32 = torch.bfloat16, torch.float32
+    x, u, (c, s) = strided(5, 300, f32, 3), strided(5, 300, f32, 7), f8(5, 300, 20, 2)
+    want = dict(rows=5, cols=300, type=F32, block_rows=1, x=x.data_ptr(), gated=u.data_ptr(), x_ld=303, gated_ld=307, codes=c.data_ptr(),
+                scales=s.data_ptr(), codes_ld=320, scales_ld=7)
+    assert fields_of(monkeypatch, lambda: B.quantize(x, u, out=(c, s))) == want
+    w = B.empty_scaled(5, 300, "cpu", 128)
+    got = fields_of(monkeypatch, lambda: B.quantize(x, block_rows=128, out=w))
+    assert got == {**want, "gated": 0, "gated_ld": 0, "block_rows": 128, "codes": w.codes.data_ptr(), "codes_ld": 304,
+                   "scales": w.scales.data_ptr(), "scales_ld": 0}
+    one = fields_of(monkeypatch, lambda: B.quantize(x[2:3], out=(c[:1], s[:, 3:4])))       # one row: its stride says nothing
+    assert one == {**want, "rows": 1, "x": x.data_ptr() + 2 * 303 * 4, "x_ld": 300, "gated": 0, "gated_ld": 0, "codes_ld": 304,
+                   "scales": s.data_ptr() + 6}
+
+    res, br, h, gate = strided(5, 300, f32, 1), strided(5, 300, bf, 2), strided(5, 300, f32, 4), strided(3, 300, bf, 5)
+    v = [torch.zeros(300, dtype=bf).as_subclass(_OnDevice) for _ in range(5)]
+    norm = dict(rows=5, d=300, type=BF16, stream_type=F32, out_type=F8, kind=B.NORM_LAYER, next_kind=B.NORM_RMS, gate_act=B.GATE_TANH,
+                gate_rows=2, eps=0.5, next_eps=0.25, weight_plus=1.0, residual_scale=2.0, residual=res.data_ptr(), branch=br.data_ptr(),
+                residual_ld=301, branch_ld=302, weight=v[0].data_ptr(), bias=v[1].data_ptr(), branch_scale=v[2].data_ptr(),
+                gate=gate.data_ptr(), gate_ld=305, next_weight=v[3].data_ptr(), next_bias=v[4].data_ptr(), h=h.data_ptr(), h_ld=304,
+                out=c.data_ptr(), out_ld=320, out_scales=s.data_ptr(), out_scales_ld=7)
+    assert fields_of(monkeypatch, lambda: B.norm_out(
+        br, res, v[0], bias=v[1], kind=B.NORM_LAYER, eps=0.5, weight_plus=1.0, residual_scale=2.0, branch_scale=v[2], gate=gate, gate_rows=2,
+        gate_act=B.GATE_TANH, next_weight=v[3], next_bias=v[4], next_kind=B.NORM_RMS, next_eps=0.25, h=h, out=(c, s))) == norm
+    n = strided(5, 300, bf, 6)
+    got = fields_of(monkeypatch, lambda: B.norm_in(res, v[3], bias=v[4], add=br, kind=B.NORM_LAYER, eps=0.25, weight_plus=1.0,
+                                                   residual_scale=2.0, h=h, out=n))
+    assert got == {**norm, "kind": 0, "next_kind": B.NORM_LAYER, "gate_act": 0, "gate_rows": 1, "eps": 0.25, "weight": 0, "bias": 0,
+                   "branch_scale": 0, "gate": 0, "gate_ld": 0, "out_type": BF16, "out": n.data_ptr(), "out_ld": 306, "out_scales": 0,
+                   "out_scales_ld": 0}
+
+    (a, sa), o = f8(5, 300, 36, 1), strided(5, 70, bf, 9)
+    w = B.Scaled(strided(70, 300, torch.float8_e4m3fn, 4), torch.zeros(1, 3))
+    mm = dict(M=5, N=70, K=300, out_type=BF16, reserved=0, a=a.data_ptr(), a_scales=sa.data_ptr(), a_ld=336, a_scales_ld=6,
+              w=w.codes.data_ptr(), w_scales=w.scales.data_ptr(), w_ld=304, c=o.data_ptr(), c_scales=0, c_ld=79, c_scales_ld=0,
+              workspace=0, workspace_bytes=B.svdmlp_scaled_matmul_workspace_bytes(5, 70, 300, BF16))
+    got = fields_of(monkeypatch, lambda: B.scaled_matmul((a, sa), w, out=o))
+    assert {**got, "workspace": 0} == mm and bool(got["workspace"]) == bool(mm["workspace_bytes"])
+    q, sq = f8(5, 70, 10, 3)
+    got = fields_of(monkeypatch, lambda: B.scaled_matmul((a, sa), w, out=(q, sq)))
+    assert {**got, "workspace": 0} == {**mm, "out_type": F8, "c": q.data_ptr(), "c_ld": 80, "c_scales": sq.data_ptr(), "c_scales_ld": 5,
+                                       "workspace_bytes": B.svdmlp_scaled_matmul_workspace_bytes(5, 70, 300, F8)}
+    a8, w8 = f8(8, 4096, 0, 0), B.empty_scaled(256, 4096, "cpu", 128)
+    got = fields_of(monkeypatch, lambda: B.scaled_matmul(a8, w8))
+    assert got["workspace"] and got["workspace_bytes"] == B.svdmlp_scaled_matmul_workspace_bytes(8, 256, 4096, BF16) > 0
+    for call in (lambda: B.quantize(x[:0]), lambda: B.norm_in(res[:0]), lambda: B.scaled_matmul((a[:0], sa[:, :0]), w)):
+        assert fields_of(monkeypatch, call) is None
 
 
 def test_scales_that_a_stride_repeats_are_refused(monkeypatch):
@@ -205,7 +277,13 @@ def test_scales_that_a_stride_repeats_are_refused(monkeypatch):
             B.quantize(fake(4, 256), out=(good.codes, scales))
         with pytest.raises(B.SvdMlpError):
             B.norm_in(fake(4, 256), out=(good.codes, scales))
-    assert B._codes((good.codes[:1], good.scales[:, 1:2]), "a", (1, 256), -1)[3] == 4      # one row of many: a stride as any
+
+
+def test_a_missing_build_is_an_error(monkeypatch, tmp_path):
+    monkeypatch.setattr(B, "_checks", None)
+    monkeypatch.setattr(B, "TENSORS_PATH", tmp_path / "nope.so")
+    with pytest.raises(FileNotFoundError):
+        B.quantize(fake(4, 256), out=B.empty_scaled(4, 256, "cpu"))
 
 
 def test_a_call_on_another_device_makes_it_current(monkeypatch):
@@ -227,8 +305,9 @@ def test_a_call_on_another_device_makes_it_current(monkeypatch):
     monkeypatch.setattr(torch.cuda, "device", on)
     monkeypatch.setattr(B, "_current_raw_stream", lambda index: 100 + index)
     monkeypatch.setattr(B, "lib", lambda: types.SimpleNamespace(op=lambda args, stream: seen.append((now[0], stream)) or 0))
-    B._run("op", 1, b"", 1)
-    B._run("op", 1, b"", 0)
+    B._run("op", b"", 1)
+    B._run("op", b"", 0)
+    B._run("op", None, 0)          # a call of no rows
     assert seen == [(1, 101), (0, 100)] and now == [0]
 
 
