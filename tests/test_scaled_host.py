@@ -252,9 +252,9 @@ def test_what_the_binding_hands_over(monkeypatch):
     got = fields_of(monkeypatch, lambda: B.scaled_matmul((a, sa), w, out=(q, sq)))
     assert {**got, "workspace": 0} == {**mm, "out_type": F8, "c": q.data_ptr(), "c_ld": 80, "c_scales": sq.data_ptr(), "c_scales_ld": 5,
                                        "workspace_bytes": B.svdmlp_scaled_matmul_workspace_bytes(5, 70, 300, F8)}
-    a8, w8 = f8(8, 4096, 0, 0), B.empty_scaled(256, 4096, "cpu", 128)
-    got = fields_of(monkeypatch, lambda: B.scaled_matmul(a8, w8))
-    assert got["workspace"] and got["workspace_bytes"] == B.svdmlp_scaled_matmul_workspace_bytes(8, 256, 4096, BF16) > 0
+    a8, w8 = f8(16, 14336, 0, 0), B.empty_scaled(512, 14336, "cpu", 128)
+    got = fields_of(monkeypatch, lambda: B.scaled_matmul(a8, w8, out_dtype=torch.float8_e4m3fn))
+    assert got["workspace"] and got["workspace_bytes"] == B.svdmlp_scaled_matmul_workspace_bytes(16, 512, 14336, F8) > 0
     for call in (lambda: B.quantize(x[:0]), lambda: B.norm_in(res[:0]), lambda: B.scaled_matmul((a[:0], sa[:, :0]), w)):
         assert fields_of(monkeypatch, call) is None
 
