@@ -61,7 +61,7 @@ __device__ __forceinline__ i32x8 block_codes(const char* row, int b, int g, int 
 // ---- up to 16 rows ------------------------------------------------------------------------------------
 // The weights go from HBM straight into registers, once.  A workgroup has 16 columns and a range of the contraction, whose
 // blocks go to its eight waves in turn, four at a time, all loads before the first product; the waves' sums meet in LDS.  One
-// row by W[4096, 4096] takes 6.1 us in a graph, by W[8192, 4096] 8.5 us (5.6 TB/s without the 2.5 us of a launch with one
+// row by W[4096, 4096] takes 6.3 us in a graph, by W[8192, 4096] 8.7 us (5.4 TB/s without the 2.5 us of a launch with one
 // load in it); two column tiles a workgroup 7.6 and 8.4 us, sixteen waves 6.3 and 8.5 us.
 constexpr int FEW_WAVES = 8;
 __global__ __launch_bounds__(64 * FEW_WAVES) void k_mm_few(MmP p) {
@@ -124,7 +124,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void k_mm_few(MmP p) {
 
 // ---- a wave's piece of the result ---------------------------------------------------------------------
 // 16 MT rows from m0 and 16 NT columns from n0 on: lane l has, of its MT rows m0 + MT (l % 16) + i, the columns 16 j + 4 (l / 16) +
-// 0..3, to be rounded or (PARTS, where there is a buffer for them) added up later.  It passes through LDS (MmResult::BYTES for each wave, free to use) so that rows leave in pieces of 32 NT bytes.
+// 0..3, to be rounded or (PARTS, where there is a buffer for them) added up later.  It passes through LDS (MmResult::BYTES for
+// each wave, free to use) so that rows leave in pieces of 32 NT bytes.
 template <int MT, int NT>
 struct MmResult {
   static constexpr int ROWS = MT < 4 ? 16 * MT : 64, LD = 32 * NT + 16;       // rows at a time, bytes per row
@@ -278,6 +279,11 @@ __device__ __forceinline__ void wait_copies(int t, int steps) {
 // has read those of step t - 1 itself) and its share of the rows of W of step t + 2 (three buffers: the second half read those
 // of step t - 1 in phase 2 t - 1).  Before a step it waits for its A, in the middle of one for its share of the next W,
 // which the first half reads in the next phase.
+//
+// Bound by the matrix cores at the clock that they hold under power: 4096 x 8192 x 16384 (rows, contraction, columns) takes
+// 445 us = 2.47 PFLOP/s, the same on zeros 364 us (3.0 PFLOP/s); in step, without the half step between them, 486 us.  4096 x 4096 x
+// 4096, one tile a CU, takes 60 us = 2.29 PFLOP/s: a tile's first copies and its result, 5 us, stand alone there.
+// PARTS: the workgroup sums a range of the contraction, where tiles are fewer than CUs and the contraction is long.
 template <int MT, int NT, int WM, int WN>
 struct MmTile {
   static constexpr int TM = 16 * MT * WM, TN = 16 * NT * WN, WAVES = WM * WN, HALF = WAVES / 2;
@@ -287,21 +293,23 @@ struct MmTile {
   static_assert(WAVES * MmResult<MT, NT>::BYTES <= LDS, "the result passes through the same memory");
 };
 
-template <int MT, int NT, int WM, int WN>
+template <int MT, int NT, int WM, int WN, bool PARTS>
 __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_mm_tile(MmP p) {
   using T = MmTile<MT, NT, WM, WN>;
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / WN, wn = wave % WN, half = wave / T::HALF;
   const int mtiles = (p.M + T::TM - 1) / T::TM, ntiles = (p.N + T::TN - 1) / T::TN;
+  const int id = xcd_contiguous_id(blockIdx.x, gridDim.x), z = PARTS ? __builtin_amdgcn_readfirstlane(id / (mtiles * ntiles)) : 0;
   int mt, nt;
-  banded_tile(xcd_contiguous_id(blockIdx.x, gridDim.x), mtiles, ntiles, p.band, mt, nt);
+  banded_tile(id - z * mtiles * ntiles, mtiles, ntiles, p.band, mt, nt);
   // divisions are done by the vector unit; copies take their addresses from scalar registers
   const int m0 = __builtin_amdgcn_readfirstlane(mt) * T::TM, n0 = __builtin_amdgcn_readfirstlane(nt) * T::TN;
   const unsigned lds0 = lds_offset_of(lds);
   // A block that ends inside comes first, so that only the prologue has to clear what lies behind it.
-  const int steps = p.KB, tail = p.K % SCALE_BLOCK;
-  auto block_of = [&](int t) { return !tail ? t : t == 0 ? steps - 1 : t - 1; };
+  const int b0 = PARTS ? z * p.range_blocks : 0, b1 = PARTS ? min(b0 + p.range_blocks, p.KB) : p.KB;
+  const int steps = b1 - b0, tail = b1 == p.KB ? p.K % SCALE_BLOCK : 0;
+  auto block_of = [&](int t) { return !tail ? b0 + t : t == 0 ? b1 - 1 : b0 + t - 1; };
 
   // Which row of A is which row of LDS: a lane has row r of each of a wave's MT tiles of 16, and those are MT consecutive rows of
   // the matrix, so that it gets their scales in one load.
@@ -438,7 +446,7 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2,
   for (int q = Q - LAG; q < Q; ++q) add(q, s_last);
 
   lds_barrier();      // everyone has read the last step
-  mm_result<MT, NT, false>(p, acc, 0, m0 + arow, n0 + wrow, wave, lds);
+  mm_result<MT, NT, PARTS>(p, acc, z, m0 + arow, n0 + wrow, wave, lds);
 }
 
 // ---- small tiles, three steps in LDS ------------------------------------------------------------------
@@ -458,7 +466,7 @@ __device__ __forceinline__ void copy_word(const char* sbase, unsigned v, unsigne
 // is multiplied, the copies of two more are on their way (three to seven made no difference), addresses are advanced and not
 // computed, and the scales come by copies as well (4 bytes for each row of A, the weights' scale 64 times), since a wait for a
 // load into a register would wait for the copies issued before it.  Rows x contraction x columns in a graph: 32 x 4096 x 14336
-// 11.4 us (6.6 TB/s of weights without the 2.5 us of a launch), 128 x 2048 x 8192 8.7 us, 256 x 4096 x 4096 13.9 us.
+// 11.9 us (6.2 TB/s of weights without the 2.5 us of a launch), 128 x 2048 x 8192 8.8 us, 256 x 4096 x 4096 13.4 us.
 constexpr int STAGES = 3;
 template <int MT, int NT>
 struct MmRing {
@@ -476,10 +484,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / 2, wn = wave % 2;
   const int mtiles = (p.M + T::TM - 1) / T::TM, ntiles = (p.N + T::TN - 1) / T::TN, tiles = mtiles * ntiles;
-  // row tiles of the same columns side by side on an XCD, whose L2 then serves the weights to all but the first
-  const int id = xcd_contiguous_id(blockIdx.x, gridDim.x), z = __builtin_amdgcn_readfirstlane(id / tiles);
-  const int nt = __builtin_amdgcn_readfirstlane((id - z * tiles) / mtiles);
-  const int m0 = (id - z * tiles - nt * mtiles) * T::TM, n0 = nt * T::TN;
+  // The tiles that share a strip of the larger operand run side by side on an XCD, whose L2 then serves it to all but the first.
+  const int id = xcd_contiguous_id(blockIdx.x, gridDim.x), z = __builtin_amdgcn_readfirstlane(id / tiles), in_z = id - z * tiles;
+  const int along = p.M > p.N ? ntiles : mtiles, strip = __builtin_amdgcn_readfirstlane(in_z / along), at = in_z - strip * along;
+  const int m0 = (p.M > p.N ? strip : at) * T::TM, n0 = (p.M > p.N ? at : strip) * T::TN;
   const int b0 = z * p.range_blocks, b1 = min(b0 + p.range_blocks, p.KB);
   const unsigned lds0 = lds_offset_of(lds);
   const int steps = b1 - b0, tail = b1 == p.KB ? p.K % SCALE_BLOCK : 0;
@@ -622,12 +630,17 @@ __global__ __launch_bounds__(256) void k_mm_join(MmP p) {
 // workgroup's steps take `step` us where it has a CU to itself (its own chain of waits), `pair` where it shares it with another,
 // `share` each where more do (the CU's copies and matrix products; below one a CU, the chip's share of them), a tile besides
 // `tile` us for its first copies and its result, a launch LAUNCH_US; cut contractions and 8-bit results of 64-column tiles add
-// a second launch that reads the partial sums.  The figures are fitted to launches in a graph.  Over 7400 sizes of 1 - 8192 rows,
-// 100 - 16384 columns and contractions, times the chosen kernel took over those of the fastest: 1.013 in the geometric mean,
-// 1.40 at most.  Model / measured us of the chosen and of others, rows x contraction x columns:
-//   16 x 4096 x 14336   ring 32x64 11.2 / 11.3, few 14.6 / 12.7       256 x 4096 x 4096    ring 64x64 14.0 / 13.9, ring 64x128 18 / 18
-//   1024 x 4096 x 4096  ring 64x128 26.9 / 28.7, tile 128x256 34 / 32   2048 x 4096 x 4096   tile 128x256 38 / 37, tile 256x256 52 / 47
-//   4096 x 4096 x 4096  tile 256x256 61 / 61, tile 128x256 74 / 71     4096 x 8192 x 16384  tile 256x256 449 / 440, tile 128x256 529 / 579
+// a second launch that reads the partial sums.  The figures are fitted to 8700 random sizes of 1 - 8192 rows, 100 - 16384 columns
+// and contractions, every kernel with the model's ranges and the next to them, in a graph; over 9400 others the times of the chosen
+// over those of the fastest were 1.006 in the geometric mean, 1.27 at most.  Model / measured us of the chosen and of others, rows x
+// contraction x columns:
+//   16 x 4096 x 14336   ring 32x64 10.9 / 11.9, few 16.5 / 17.9         256 x 4096 x 4096   ring 32x64 12.4 / 13.4, ring 64x64 13.7 / 14.1
+//   1024 x 4096 x 4096  ring 64x128 22.9 / 26.0, tile 128x256 in 2 ranges 37.8 / 32.3
+//   2048 x 4096 x 4096  tile 128x256 38.4 / 37.0, tile 256x256 53.7 / 47.4
+//   4096 x 4096 x 4096  tile 256x256 59.1 / 60.0, tile 128x256 69.8 / 72.9
+//   4096 x 8192 x 16384 tile 256x256 434 / 446, tile 128x256 540 / 560
+//   286 x 13184 x 7424  tile 256x256 in 4 ranges 62 / 58, in one 148 / 143
+//   4096 x 14336 x 512  ring 64x64 45 / 50, tile 128x256 in 4 ranges 50 / 44, in one 105 / 93
 // (Further tiles measured and not kept: 128 x 128 with four waves, 256 x 128, 128 x 64, 32 x 128: level or behind one of these.)
 enum { MM_FEW = 0, MM_RING_32, MM_RING_64, MM_RING_64_128, MM_TILE_128_256, MM_TILE_256, MM_KINDS };
 struct MmKind {
@@ -636,14 +649,14 @@ struct MmKind {
   double step, pair, share, tile;
 };
 constexpr MmKind MM_KIND[MM_KINDS] = {
-    {"k_mm_few[tile=16x16", 16, 16, 16, 0.62 / FEW_WAVES, 1.20 / FEW_WAVES, 0.60 / FEW_WAVES, 0.},
-    {"k_mm_ring[tile=32x64", 32, 64, 0, 0.26, 0.34, 0.17, 0.4},
-    {"k_mm_ring[tile=64x64", 64, 64, 0, 0.34, 0.40, 0.255, 0.6},
-    {"k_mm_ring[tile=64x128", 64, 128, 0, 0.45, 0.70, 0.36, 1.0},
-    {"k_mm_tile[tile=128x256", 128, 256, 0, 0.87, 2.0, 1.0, 3.5},
-    {"k_mm_tile[tile=256x256", 256, 256, 0, 1.35, 3.3, 1.65, 6.0},
+    {"k_mm_few[tile=16x16", 16, 16, 16, 0.57 / FEW_WAVES, 1.09 / FEW_WAVES, 0.545 / FEW_WAVES, 0.},
+    {"k_mm_ring[tile=32x64", 32, 64, 0, 0.24, 0.28, 0.174, 0.46},
+    {"k_mm_ring[tile=64x64", 64, 64, 0, 0.33, 0.366, 0.268, 0.65},
+    {"k_mm_ring[tile=64x128", 64, 128, 0, 0.485, 0.577, 0.393, 0.98},
+    {"k_mm_tile[tile=128x256", 128, 256, 0, 1.02, 1.9, 1.0, 3.25},
+    {"k_mm_tile[tile=256x256", 256, 256, 0, 1.43, 3.1, 1.6, 5.4},
 };
-constexpr double LAUNCH_US = 2.5, JOIN_US = 2.3, JOIN_RANGE_US = 0.1, HBM_BYTES_PER_US = 6.8e6, PART_BYTES_PER_US = 4.0e6;
+constexpr double LAUNCH_US = 2.5, JOIN_US = 2.6, JOIN_RANGE_US = 0.1, HBM_BYTES_PER_US = 7.05e6, PART_BYTES_PER_US = 5.2e6;
 constexpr int MM_CUS = 256;      // the model's device, so that a result's order of sums goes by the extents alone
 
 struct MmPlan {
@@ -663,7 +676,8 @@ static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, MmPlan* best) 
     const MmKind& kind = MM_KIND[k];
     if (kind.max_rows && M > kind.max_rows) continue;
     const int64_t tiles = ((M + kind.rows - 1) / kind.rows) * ((N + kind.cols - 1) / kind.cols);
-    for (int r = 1; r <= (k < MM_TILE_128_256 ? 32 : 1) && r <= KB; r *= 2) {     // the tile kernels take whole contractions
+    const bool large = k >= MM_TILE_128_256;
+    for (int r = 1; r <= (large ? 8 : 32) && r <= KB; r += !large ? r : r < 4 ? 1 : 2) {
       MmPlan q;
       q.kind = k;
       q.tiles = tiles;
@@ -680,11 +694,11 @@ static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, MmPlan* best) 
       double hbm = ((double)N * K + (double)M * K + (double)M * N * (out_type == SVDMLP_F8 ? 1 : 2)) / HBM_BYTES_PER_US;
       if (k == MM_FEW) {          // eight waves take a block each; every workgroup reads the rows of A
         steps = (steps + FEW_WAVES - 1) / FEW_WAVES * FEW_WAVES;
-        step += 0.022 / FEW_WAVES * M * per_cu;
+        step += 0.0205 / FEW_WAVES * M * per_cu;
       }
       if (!on_lines) {
-        step *= k == MM_TILE_256 ? 1.05 : 1.25;
-        hbm *= 1.3;
+        step *= k == MM_TILE_256 ? 1.07 : 1.28;
+        hbm *= 1.84;
       }
       double t = kind.tile * per_cu + steps * step;
       if (t < hbm) t = hbm;
@@ -713,6 +727,11 @@ static void launch_join(const MmP& p, hipStream_t st) {
   }
 }
 
+template <int MT>
+static void launch_tile(const MmP& p, unsigned wgs, hipStream_t st) {
+  if (p.part) k_mm_tile<MT, 4, 2, 4, true><<<wgs, 512, 0, st>>>(p);
+  else k_mm_tile<MT, 4, 2, 4, false><<<wgs, 512, 0, st>>>(p);
+}
 static void launch_mm(MmP& p, const MmPlan& q, hipStream_t st) {
   const unsigned wgs = (unsigned)(q.tiles * q.ranges);
   p.band = band_height((p.M + MM_KIND[q.kind].rows - 1) / MM_KIND[q.kind].rows, wgs);
@@ -721,8 +740,8 @@ static void launch_mm(MmP& p, const MmPlan& q, hipStream_t st) {
     case MM_RING_32: k_mm_ring<1, 2><<<wgs, 256, 0, st>>>(p); break;
     case MM_RING_64: k_mm_ring<2, 2><<<wgs, 256, 0, st>>>(p); break;
     case MM_RING_64_128: k_mm_ring<2, 4><<<wgs, 256, 0, st>>>(p); break;
-    case MM_TILE_128_256: k_mm_tile<4, 4, 2, 4><<<wgs, 512, 0, st>>>(p); break;
-    default: k_mm_tile<8, 4, 2, 4><<<wgs, 512, 0, st>>>(p); break;
+    case MM_TILE_128_256: launch_tile<4>(p, wgs, st); break;
+    default: launch_tile<8>(p, wgs, st); break;
   }
 }
 

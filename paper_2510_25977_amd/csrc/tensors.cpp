@@ -1,6 +1,5 @@
 // The binding's checks of torch tensors, and the argument structures of the 8-bit operators made from them.  The smallest calls
-// are bound by the host: a launch takes it 3.1 us, checking the six tensors of a norm in Python and packing their addresses 4 more;
-// here that is 0.3.
+// are bound by the host, where a launch alone takes 3.1 us: a norm of six tensors 5.0 in all, 7.8 with the checks in Python.
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 

@@ -123,7 +123,7 @@ MATMULS = [
     (16, 300, 129), (31, 128, 255), (32, 257, 256), (33, 96, 257), (47, 200, 640), (64, 512, 1000), (1, 1000, 2304),
     (63, 33, 3000), (65, 384, 513), (100, 127, 2000), (128, 256, 384), (129, 255, 383), (200, 520, 1152), (256, 256, 512),
     (257, 640, 300), (300, 1000, 270), (513, 515, 517), (1000, 700, 1100), (40, 3000, 400), (2, 16, 9000), (130, 40, 9001), (7, 9, 3000),
-    (20, 15, 5000), (1, 131, 4000), (64, 259, 4000),
+    (20, 15, 5000), (1, 131, 4000), (64, 259, 4000), (1036, 9, 3647), (2993, 131, 5942), (168, 5463, 7852), (129, 5770, 7063),
     # what else the product's kernels and their cuts of the contraction are chosen for (a host test sees to it that all are here)
     (3, 6000, 300), (700, 500, 1300), (520, 300, 2500), (700, 4100, 400), (90, 1100, 4000), (2741, 2252, 135), (1301, 4999, 300),
     (1290, 5000, 513), (300, 2600, 6000), (2100, 5000, 257), (2111, 4983, 600), (1500, 600, 9000), (3, 66, 555), (284, 1738, 1842),

@@ -132,16 +132,16 @@ def test_the_gpu_tests_sizes_reach_every_kernel_of_the_product():
             d = B.svdmlp_scaled_matmul_describe(M, N, K, out)
             seen.add((re.match(r"k_mm_\w+\[tile=\d+x\d+", d).group(0), "ranges=1 " in d, out))
             assert ("k_mm_join" in d) == (B.svdmlp_scaled_matmul_workspace_bytes(M, N, K, out) > 0)
-    few_and_rings = ["k_mm_few[tile=16x16", "k_mm_ring[tile=32x64", "k_mm_ring[tile=64x64", "k_mm_ring[tile=64x128"]
-    want = {(k, whole, out) for k in few_and_rings for whole in (True, False) for out in (BF16, F8)}
-    want |= {(k, True, out) for k in ("k_mm_tile[tile=128x256", "k_mm_tile[tile=256x256") for out in (BF16, F8)}
-    assert seen == want
+    kernels = ["k_mm_few[tile=16x16", "k_mm_ring[tile=32x64", "k_mm_ring[tile=64x64", "k_mm_ring[tile=64x128", "k_mm_tile[tile=128x256",
+               "k_mm_tile[tile=256x256"]
+    assert seen == {(k, whole, out) for k in kernels for whole in (True, False) for out in (BF16, F8)}
 
 
 @pytest.mark.parametrize("M,N,K,kernel", [
     (1, 4096, 4096, "few"), (16, 4096, 4096, "few"), (1, 14336, 4096, "ring[tile=32x64"), (16, 14336, 4096, "ring[tile=32x64"),
-    (128, 8192, 2048, "ring[tile=64x64"), (256, 4096, 4096, "ring[tile=64x64"), (1024, 4096, 4096, "ring[tile=64x128"),
-    (512, 14336, 4096, "tile[tile=128x256"), (2048, 4096, 4096, "tile[tile=128x256"), (1777, 7301, 2687, "tile[tile=256x256"), (4096, 16384, 8192, "tile[tile=256x256"),
+    (128, 8192, 2048, "ring[tile=32x64"), (256, 4096, 4096, "ring[tile=32x64"), (300, 4096, 8192, "ring[tile=64x64"),
+    (1024, 4096, 4096, "ring[tile=64x128"), (512, 14336, 4096, "tile[tile=128x256"), (2048, 4096, 4096, "tile[tile=128x256"),
+    (1777, 7301, 2687, "tile[tile=256x256"), (4096, 16384, 8192, "tile[tile=256x256"), (286, 7424, 13184, "tile[tile=256x256 tiles=58 ranges=4"),
 ])
 def test_the_products_planner_takes_what_measured_fastest(M, N, K, kernel):
     assert B.svdmlp_scaled_matmul_describe(M, N, K, BF16).startswith("k_mm_" + kernel)
