@@ -28,9 +28,15 @@ struct MmP {
   int64_t a_ld, w_ld, sa_ld, c_ld, c_scales_ld;
   int M, N, K, KB;
   int out_type;
-  int band;                   // row tiles of a band of banded_tile
+  int tiles;                  // of the result
+  int band;                   // k_mm_tile: row tiles of a band of banded_tile; k_mm_ring: tiles of a strip
   int ranges, range_blocks;   // ranges of the contraction, blocks of 128 in each (the last may be shorter)
 };
+
+// Workgroups sum range after range of the contraction.  A division is 0.1 us before a workgroup's first load: left out where it can be.
+__device__ __forceinline__ int range_of(int id, const MmP& p) {
+  return p.ranges == 1 ? 0 : __builtin_amdgcn_readfirstlane(id / p.tiles);
+}
 
 __device__ __forceinline__ f32x4 mfma_f8(const i32x8& w, const i32x8& a, f32x4 c) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, 0, 0, 0);
@@ -61,14 +67,14 @@ __device__ __forceinline__ i32x8 block_codes(const char* row, int b, int g, int 
 // ---- up to 16 rows ------------------------------------------------------------------------------------
 // The weights go from HBM straight into registers, once.  A workgroup has 16 columns and a range of the contraction, whose
 // blocks go to its eight waves in turn, four at a time, all loads before the first product; the waves' sums meet in LDS.  One
-// row by W[4096, 4096] takes 6.3 us in a graph, by W[8192, 4096] 8.7 us (5.4 TB/s without the 2.5 us of a launch with one
+// row by W[4096, 4096] takes 6.2 us in a graph, by W[8192, 4096] 8.7 us (5.4 TB/s without the 2.5 us of a launch with one
 // load in it); two column tiles a workgroup 7.6 and 8.4 us, sixteen waves 6.3 and 8.5 us.
 constexpr int FEW_WAVES = 8;
 __global__ __launch_bounds__(64 * FEW_WAVES) void k_mm_few(MmP p) {
   __shared__ f32x4 red[FEW_WAVES][64];
   const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int ntiles = (p.N + 15) / 16, z = blockIdx.x / ntiles, n0 = (blockIdx.x - z * ntiles) * 16;
+  const int z = range_of(blockIdx.x, p), n0 = (blockIdx.x - z * p.tiles) * 16;
   const char* wr = p.w + (int64_t)min(n0 + r, p.N - 1) * p.w_ld;
   const char* ar = p.a + min(r, p.M - 1) * p.a_ld;
   const __bf16* sa = p.sa + min(r, p.M - 1);
@@ -300,9 +306,9 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2,
   const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / WN, wn = wave % WN, half = wave / T::HALF;
   const int mtiles = (p.M + T::TM - 1) / T::TM, ntiles = (p.N + T::TN - 1) / T::TN;
-  const int id = xcd_contiguous_id(blockIdx.x, gridDim.x), z = PARTS ? __builtin_amdgcn_readfirstlane(id / (mtiles * ntiles)) : 0;
+  const int id = xcd_contiguous_id(blockIdx.x, gridDim.x), z = PARTS ? range_of(id, p) : 0;
   int mt, nt;
-  banded_tile(id - z * mtiles * ntiles, mtiles, ntiles, p.band, mt, nt);
+  banded_tile(id - z * p.tiles, mtiles, ntiles, p.band, mt, nt);
   // divisions are done by the vector unit; copies take their addresses from scalar registers
   const int m0 = __builtin_amdgcn_readfirstlane(mt) * T::TM, n0 = __builtin_amdgcn_readfirstlane(nt) * T::TN;
   const unsigned lds0 = lds_offset_of(lds);
@@ -466,7 +472,7 @@ __device__ __forceinline__ void copy_word(const char* sbase, unsigned v, unsigne
 // is multiplied, the copies of two more are on their way (three to seven made no difference), addresses are advanced and not
 // computed, and the scales come by copies as well (4 bytes for each row of A, the weights' scale 64 times), since a wait for a
 // load into a register would wait for the copies issued before it.  Rows x contraction x columns in a graph: 32 x 4096 x 14336
-// 11.9 us (6.2 TB/s of weights without the 2.5 us of a launch), 128 x 2048 x 8192 8.8 us, 256 x 4096 x 4096 13.4 us.
+// 11.3 us (6.7 TB/s of weights without the 2.5 us of a launch), 128 x 2048 x 8192 8.5 us, 256 x 4096 x 4096 13.0 us.
 constexpr int STAGES = 3;
 template <int MT, int NT>
 struct MmRing {
@@ -483,10 +489,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / 2, wn = wave % 2;
-  const int mtiles = (p.M + T::TM - 1) / T::TM, ntiles = (p.N + T::TN - 1) / T::TN, tiles = mtiles * ntiles;
   // The tiles that share a strip of the larger operand run side by side on an XCD, whose L2 then serves it to all but the first.
-  const int id = xcd_contiguous_id(blockIdx.x, gridDim.x), z = __builtin_amdgcn_readfirstlane(id / tiles), in_z = id - z * tiles;
-  const int along = p.M > p.N ? ntiles : mtiles, strip = __builtin_amdgcn_readfirstlane(in_z / along), at = in_z - strip * along;
+  const int id = xcd_contiguous_id(blockIdx.x, gridDim.x), z = range_of(id, p), in_z = id - z * p.tiles;
+  const int strip = __builtin_amdgcn_readfirstlane(in_z / p.band), at = in_z - strip * p.band;
   const int m0 = (p.M > p.N ? strip : at) * T::TM, n0 = (p.M > p.N ? at : strip) * T::TN;
   const int b0 = z * p.range_blocks, b1 = min(b0 + p.range_blocks, p.KB);
   const unsigned lds0 = lds_offset_of(lds);
@@ -634,7 +639,7 @@ __global__ __launch_bounds__(256) void k_mm_join(MmP p) {
 // and contractions, every kernel with the model's ranges and the next to them, in a graph; over 9400 others the times of the chosen
 // over those of the fastest were 1.006 in the geometric mean, 1.27 at most.  Model / measured us of the chosen and of others, rows x
 // contraction x columns:
-//   16 x 4096 x 14336   ring 32x64 10.9 / 11.9, few 16.5 / 17.9         256 x 4096 x 4096   ring 32x64 12.4 / 13.4, ring 64x64 13.7 / 14.1
+//   16 x 4096 x 14336   ring 32x64 10.9 / 11.3, few 16.5 / 17.9         256 x 4096 x 4096   ring 32x64 12.4 / 13.0, ring 64x64 13.7 / 14.1
 //   1024 x 4096 x 4096  ring 64x128 22.9 / 26.0, tile 128x256 in 2 ranges 37.8 / 32.3
 //   2048 x 4096 x 4096  tile 128x256 38.4 / 37.0, tile 256x256 53.7 / 47.4
 //   4096 x 4096 x 4096  tile 256x256 59.1 / 60.0, tile 128x256 69.8 / 72.9
@@ -734,7 +739,10 @@ static void launch_tile(const MmP& p, unsigned wgs, hipStream_t st) {
 }
 static void launch_mm(MmP& p, const MmPlan& q, hipStream_t st) {
   const unsigned wgs = (unsigned)(q.tiles * q.ranges);
-  p.band = band_height((p.M + MM_KIND[q.kind].rows - 1) / MM_KIND[q.kind].rows, wgs);
+  const MmKind& kind = MM_KIND[q.kind];
+  const int mtiles = (p.M + kind.rows - 1) / kind.rows, ntiles = (p.N + kind.cols - 1) / kind.cols;
+  p.tiles = (int)q.tiles;
+  p.band = q.kind >= MM_TILE_128_256 ? band_height(mtiles, wgs) : p.M > p.N ? ntiles : mtiles;
   switch (q.kind) {
     case MM_FEW: k_mm_few<<<wgs, 64 * FEW_WAVES, 0, st>>>(p); break;
     case MM_RING_32: k_mm_ring<1, 2><<<wgs, 256, 0, st>>>(p); break;
