@@ -308,8 +308,8 @@ enum { SVDMLP_GATE_PLAIN = 0, SVDMLP_GATE_SIGMOID = 1, SVDMLP_GATE_TANH = 2 };
  * Sums, h and both norms are fp32; the second norm takes h before it is rounded to its type.  A norm that is given no
  * weight or bias leaves it out; likewise branch_scale and gate.  Each row is read whole before any of it is written, so h
  * may be the residual's own buffer (same pointer and stride); otherwise outputs must not overlap inputs.
- * d: 1 .. 32768, fewer than 2^25 rows up to d = 512, 2^23 up to 2048, 2^22 up to 16384, 2^21 beyond (else
- * SVDMLP_UNSUPPORTED).  type / stream_type: BF16 / BF16, BF16 / F32 or F32 / F32. */
+ * d: 1 .. 32768, fewer than 2^25 rows up to d = 512, 2^24 up to 1024, 2^23 up to 2048, 2^22 up to 16384,
+ * 2^21 beyond (else SVDMLP_UNSUPPORTED).  type / stream_type: BF16 / BF16, BF16 / F32 or F32 / F32. */
 typedef struct {
   int64_t rows, d;
   int32_t type;             /* of branch, gate, every weight, and of out unless that is 8-bit */

@@ -11,8 +11,9 @@ struct NormP {
   const void *residual, *branch, *weight, *bias, *branch_scale, *gate, *next_weight, *next_bias;
   void *h, *out;
   __bf16* out_scales;
-  int64_t residual_ld, branch_ld, gate_ld, h_ld, out_ld, out_scales_ld, gate_rows;
+  int64_t residual_ld, branch_ld, gate_ld, h_ld, out_ld, out_scales_ld;
   int64_t rows;
+  unsigned gate_rows;
   int d, kind, next_kind, gate_act, out_f8;
   float eps, next_eps, weight_plus, residual_scale, inv_d;
 };
@@ -72,17 +73,20 @@ __device__ __forceinline__ float activated(float g, int act) {
 
 // TPR threads hold a row, thread t columns 8 (i TPR + t) .. + 7, i < NV: 16 lanes hold a block of 128 columns.  Weights come with the
 // row up to two vectors a thread (4096 x 4096 26.3 us, 30.6 after the row's sum), with four they come when they are needed: the
-// registers allow half the waves otherwise (2048 x 16384 with gate and fp32 residual 102 us, 121; 2048 x 32768 fp32 136, 295).
+// registers allow half the waves otherwise (2048 x 16384 with gate and fp32 residual 102 us, 121; 2048 x 32768 fp32 136, 295).  At
+// one vector of bf16 the biases, the scale and the gate come along too (3616 x 3968 with all of them 33.0 us, 35.5 later).
 template <class T, class S, int TPR, int NV, RowEnd END>
 __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
   constexpr int WAVES = TPR / 64;
-  constexpr bool EARLY = NV < 4;      // weights loaded with the row
+  constexpr bool EARLY = NV < 4;                         // weights loaded with the row,
+  constexpr bool ALL_EARLY = NV == 1 && sizeof(T) == 2;  // and whatever else there is
   __shared__ float part[4 * WAVES];
   const int t = threadIdx.x % TPR;
   const int64_t row = (int64_t)blockIdx.x * (TPR == 64 ? 4 : 1) + threadIdx.x / TPR;
   if (row >= p.rows) return;   // whole waves, and whole workgroups where they meet at a barrier
-  Raw8<T> rb[NV], w[NV], nw[NV];
+  Raw8<T> rb[NV], w[NV], nw[NV], bias[NV], bscale[NV], gate[NV], nbias[NV];
   Raw8<S> rr[NV];
+  const T* gate_row = (const T*)p.gate + (int64_t)((unsigned)row / p.gate_rows) * p.gate_ld;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const Cols<END> k((i * TPR + t) * 8, p.d);
@@ -91,6 +95,12 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
     if (EARLY) {
       w[i] = p.weight ? load8((const T*)p.weight, k) : Raw8<T>{};
       nw[i] = p.next_weight ? load8((const T*)p.next_weight, k) : Raw8<T>{};
+    }
+    if (ALL_EARLY) {
+      bias[i] = p.bias ? load8((const T*)p.bias, k) : Raw8<T>{};
+      bscale[i] = p.branch_scale ? load8((const T*)p.branch_scale, k) : Raw8<T>{};
+      gate[i] = p.gate ? load8(gate_row, k) : Raw8<T>{};
+      nbias[i] = p.next_bias ? load8((const T*)p.next_bias, k) : Raw8<T>{};
     }
   }
   float v[NV][8];
@@ -111,19 +121,19 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
       for (int e = 0; e < 8; ++e) v[i][e] *= w[i].get(e) + p.weight_plus;
     }
     if (p.bias) {
-      const Raw8<T> b = load8((const T*)p.bias, k);
+      if (!ALL_EARLY) bias[i] = load8((const T*)p.bias, k);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] += b.get(e);
+      for (int e = 0; e < 8; ++e) v[i][e] += bias[i].get(e);
     }
     if (p.branch_scale) {
-      const Raw8<T> s = load8((const T*)p.branch_scale, k);
+      if (!ALL_EARLY) bscale[i] = load8((const T*)p.branch_scale, k);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] *= s.get(e);
+      for (int e = 0; e < 8; ++e) v[i][e] *= bscale[i].get(e);
     }
     if (p.gate) {
-      const Raw8<T> s = load8((const T*)p.gate + row / p.gate_rows * p.gate_ld, k);
+      if (!ALL_EARLY) gate[i] = load8(gate_row, k);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] *= activated(s.get(e), p.gate_act);
+      for (int e = 0; e < 8; ++e) v[i][e] *= activated(gate[i].get(e), p.gate_act);
     }
     if (p.residual) {
 #pragma unroll
@@ -145,9 +155,9 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
       for (int e = 0; e < 8; ++e) v[i][e] *= nw[i].get(e) + p.weight_plus;
     }
     if (p.next_bias) {
-      const Raw8<T> b = load8((const T*)p.next_bias, k);
+      if (!ALL_EARLY) nbias[i] = load8((const T*)p.next_bias, k);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] += b.get(e);
+      for (int e = 0; e < 8; ++e) v[i][e] += nbias[i].get(e);
     }
     if (!p.out_f8) {
       if (k.any()) store8((T*)p.out + row * p.out_ld, k, v[i]);
@@ -177,14 +187,16 @@ static void run_norm(const NormP& p, hipStream_t st) {
 
 // As few vectors a thread as a workgroup's size allows: a row's chain (loads, sums over the workgroup, stores) is what a CU has
 // four of at 512 threads.  us in a graph, 1024 / 512 / 256 / 128 threads for the row: 4096 x 4096 in 8 bits with a residual
-// 27.6 / 26.3 / 26.3 / 28.5, one such row 5.0 / 4.6 / 4.9, 8192 x 5120 with gate and fp32 residual - / 109 / 113 / 139.
-static int row_threads(int64_t d) { return d <= 512 ? 64 : d <= 2048 ? 256 : d <= 16384 ? 512 : 1024; }
+// 27.6 / 26.3 / 26.3 / 28.5, one such row 5.0 / 4.6 / 4.9, 8192 x 5120 with gate and fp32 residual - / 109 / 113 / 139;
+// 5359 x 562 with all inputs 11.9 with 128 threads, 16.1 with 256.
+static int row_threads(int64_t d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 16384 ? 512 : 1024; }
 
 template <class T, class S>
 static void launch_norm(const NormP& p, hipStream_t st) {
   if (row_end(p.d) == SHORT) return run_norm<T, S, 64, 1, SHORT>(p, st);
   switch (row_threads(p.d)) {
     case 64: return run_norm<T, S, 64, 1>(p, st);
+    case 128: return run_norm<T, S, 128, 1>(p, st);
     case 256: return run_norm<T, S, 256, 1>(p, st);
     case 512: break;
     default: return run_norm<T, S, 1024, 4>(p, st);
@@ -234,7 +246,7 @@ extern "C" int svdmlp_norm(const svdmlp_norm_args* a, void* hip_stream) {
   p.branch_scale = a->branch_scale; p.gate = a->gate; p.next_weight = a->next_weight; p.next_bias = a->next_bias;
   p.h = a->h; p.out = a->out; p.out_scales = (__bf16*)a->out_scales;
   p.residual_ld = a->residual_ld; p.branch_ld = a->branch_ld; p.gate_ld = a->gate_ld; p.h_ld = a->h_ld; p.out_ld = a->out_ld;
-  p.out_scales_ld = a->out_scales_ld; p.gate_rows = a->gate_rows < 1 ? 1 : a->gate_rows;
+  p.out_scales_ld = a->out_scales_ld; p.gate_rows = (unsigned)(a->gate_rows < 1 ? 1 : a->gate_rows < a->rows ? a->gate_rows : a->rows);
   p.rows = a->rows; p.d = (int)a->d; p.kind = a->kind; p.next_kind = a->next_kind; p.gate_act = a->gate_act;
   p.out_f8 = next && a->out_type == SVDMLP_F8;
   p.eps = a->eps; p.next_eps = a->next_eps; p.weight_plus = a->weight_plus; p.residual_scale = a->residual_scale;
