@@ -1,7 +1,7 @@
 // The norms around a block of the residual stream, with the residual, the gate and the scales, in one pass:
 //   b = [norm(branch) (weight + plus) + bias] branch_scale act(gate)    h = residual_scale residual + b    out = norm(h) ..
 // A row lies in the registers of its threads in fp32 from its first load to its last store, so every input is read once and
-// every result written once, and HBM bounds it: 4096 x 4096 with a residual into 8 bits 117 MB in 26.3 us (4.5 TB/s; a copy of
+// every result written once, and HBM bounds it: 4096 x 4096 with a residual into 8 bits 117 MB in 25.4 us (4.6 TB/s; a copy of
 // 2 GiB moves 4.8), 8192 x 5120 with an fp32 residual 503 MB in 91 us (5.5 TB/s), with a tanh gate and scale 109 us.
 #include "scaled.h"
 
