@@ -342,13 +342,15 @@ int svdmlp_norm(const svdmlp_norm_args *args, void *hip_stream);
  * sums are added in fp32.  M, N, K are free (1 <= N, K <= 2^22, M < 2^24, fewer than 2^22 tiles of 256 x 256, else
  * SVDMLP_UNSUPPORTED); where the contraction ends inside a block the rest of the block counts as zero whatever lies there.  The order of the sums depends on the extents alone: the same call
  * gives the same bits.  C must not overlap an operand.
+ * gated: the contraction is two in a row, K / 2 each and K a multiple of 256.  The first half's sums G and the second's P stay
+ * fp32 and C = SiLU(G) .* P: the gate and up products of a block, whose operands lie side by side, in one call.
  * Some extents cut the contraction into ranges that different workgroups sum: their partial sums take
  * svdmlp_scaled_matmul_workspace_bytes bytes (0 for most; 16-byte aligned) of a workspace that is free again when the
  * call's kernels are done.  Calls that may overlap need a workspace each. */
 typedef struct {
   int64_t M, N, K;
   int32_t out_type;         /* SVDMLP_BF16 or SVDMLP_F8 */
-  int32_t reserved;         /* 0 */
+  int32_t gated;            /* 0 or 1 */
   const void *a, *a_scales;
   int64_t a_ld, a_scales_ld;
   const void *w;
@@ -360,10 +362,10 @@ typedef struct {
   size_t workspace_bytes;
 } svdmlp_scaled_matmul_args;
 int svdmlp_scaled_matmul(const svdmlp_scaled_matmul_args *args, void *hip_stream);
-size_t svdmlp_scaled_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t out_type);
+size_t svdmlp_scaled_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t out_type);   /* gated: none */
 
 /* Host only: one line naming the kernel a product of these extents takes and how it is cut (on 256 CUs). */
-int svdmlp_scaled_matmul_describe(int64_t M, int64_t N, int64_t K, int32_t out_type, char *buf, size_t buf_bytes);
+int svdmlp_scaled_matmul_describe(int64_t M, int64_t N, int64_t K, int32_t out_type, int32_t gated, char *buf, size_t buf_bytes);
 
 /* ABI version of this header (bumped on any incompatible change). */
 int svdmlp_abi_version(void);

@@ -125,8 +125,8 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).restype = ctypes.c_int
         L.svdmlp_scaled_matmul_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32]
         L.svdmlp_scaled_matmul_workspace_bytes.restype = ctypes.c_size_t
-        L.svdmlp_scaled_matmul_describe.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_char_p,
-                                                    ctypes.c_size_t]
+        L.svdmlp_scaled_matmul_describe.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                                    ctypes.c_char_p, ctypes.c_size_t]
         L.svdmlp_scaled_matmul_describe.restype = ctypes.c_int
         _lib = L
     return _lib
@@ -492,18 +492,21 @@ def svdmlp_scaled_matmul_workspace_bytes(M: int, N: int, K: int, out_type: int) 
     return int(lib().svdmlp_scaled_matmul_workspace_bytes(int(M), int(N), int(K), int(out_type)))
 
 
-def svdmlp_scaled_matmul_describe(M: int, N: int, K: int, out_type: int) -> str:
+def svdmlp_scaled_matmul_describe(M: int, N: int, K: int, out_type: int, gated: bool = False) -> str:
     buf = ctypes.create_string_buffer(512)
-    _check(lib().svdmlp_scaled_matmul_describe(int(M), int(N), int(K), int(out_type), buf, len(buf)), "svdmlp_scaled_matmul_describe")
+    _check(lib().svdmlp_scaled_matmul_describe(int(M), int(N), int(K), int(out_type), int(gated), buf, len(buf)),
+           "svdmlp_scaled_matmul_describe")
     return buf.value.decode()
 
 
-def scaled_matmul(a, w, *, out=None, out_dtype: torch.dtype = torch.bfloat16, stream: Optional[torch.cuda.Stream] = None):
+def scaled_matmul(a, w, *, gated: bool = False, out=None, out_dtype: torch.dtype = torch.bfloat16,
+                  stream: Optional[torch.cuda.Stream] = None):
     """a [M, K] times the transpose of w [N, K], both ``Scaled`` (or pairs of codes and scales): activations with a scale per
     row and 128 columns, weights with one per 128 x 128.  The result [M, N] is ``out`` or a new tensor of ``out_dtype``;
-    torch.float8_e4m3fn (or a ``Scaled`` as ``out``) makes it the next product's activations."""
+    torch.float8_e4m3fn (or a ``Scaled`` as ``out``) makes it the next product's activations.  ``gated``: the two halves of K
+    (a multiple of 256) are a gate and an up product side by side, the result SiLU(gate) * up."""
     if stream is not None:
-        return _on(stream, scaled_matmul, tuple(a), w, out=out, out_dtype=out_dtype)
+        return _on(stream, scaled_matmul, tuple(a), w, gated=gated, out=out, out_dtype=out_dtype)
     codes, scales = a
     w_codes, w_scales = w
     dev = _device_of(codes, "a")
@@ -520,9 +523,10 @@ def scaled_matmul(a, w, *, out=None, out_dtype: torch.dtype = torch.bfloat16, st
         c, c_scales = out
     else:
         c, c_scales = out, None
-    need = svdmlp_scaled_matmul_workspace_bytes(M, N, K, SVDMLP_BF16 if c_scales is None else SVDMLP_F8)
+    need = 0 if gated else svdmlp_scaled_matmul_workspace_bytes(M, N, K, SVDMLP_BF16 if c_scales is None else SVDMLP_F8)
     space = torch.empty(need, dtype=torch.uint8, device=codes.device) if need else None
-    _run("svdmlp_scaled_matmul", _tensors().scaled_matmul_args(dev, M, N, K, codes, scales, w_codes, w_scales, c, c_scales, space), dev)
+    args = _tensors().scaled_matmul_args(dev, M, N, K, codes, scales, w_codes, w_scales, c, c_scales, space, bool(gated))
+    _run("svdmlp_scaled_matmul", args, dev)
     return out
 
 
@@ -563,7 +567,7 @@ class SvdMlpF8:
             self.first, self.last = weights(ranked(Ug)), weights(rank_rows(Vg))
         else:
             self.first = weights(ranked(Ug), ranked(Uu))
-            self.gate, self.up = weights(rank_rows(Vg)), weights(rank_rows(Vu))
+            self.gate_up = quantize(torch.cat([rank_rows(Vg).t(), rank_rows(Vu).t()], 1), block_rows=SCALE_BLOCK)
             self.down, self.last = weights(ranked(Ud)), weights(rank_rows(Vd))
 
     def out_features(self) -> int:
@@ -577,11 +581,8 @@ class SvdMlpF8:
             X = quantize(X)
         T = scaled_matmul(X, self.first, out_dtype=_F8)
         if self.kind == SVDMLP_GATED:
-            rank = self.gate.codes.shape[1]
-            blocks = rank // SCALE_BLOCK
-            G = scaled_matmul(Scaled(T.codes[:, :rank], T.scales[:blocks]), self.gate)
-            P = scaled_matmul(Scaled(T.codes[:, rank:], T.scales[blocks:]), self.up)
-            T = scaled_matmul(quantize(G, P), self.down, out_dtype=_F8)
+            H = scaled_matmul(T, self.gate_up, gated=True, out_dtype=_F8)
+            T = scaled_matmul(H, self.down, out_dtype=_F8)
         return scaled_matmul(T, self.last, out=out)
 
     __call__ = forward

@@ -244,6 +244,20 @@ __device__ __forceinline__ void mm_result(const MmP& p, const f32x4 (&acc)[NT][M
   }
 }
 
+// sums <- SiLU(gate) sums
+template <int MT, int NT>
+__device__ __forceinline__ void gate_sums(f32x4 (&sums)[NT][MT], const f32x4 (&gate)[NT][MT]) {
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float g = gate[j][i][e];
+        sums[j][i][e] *= g * __builtin_amdgcn_rcpf(1.f + __expf(-g));
+      }
+}
+
 // ---- tiles through LDS ------------------------------------------------------------------------------
 // C times 16 bytes a lane, global -> LDS, if t < steps: a wave-uniform base and a 32-bit offset per lane; lane l lands at
 // lds_dst + 16 l, each copy STRIDE bytes after the one before.  The branch is inside so that the compiler sees none in the
@@ -290,6 +304,10 @@ __device__ __forceinline__ void wait_copies(int t, int steps) {
 // 445 us = 2.47 PFLOP/s, the same on zeros 364 us (3.0 PFLOP/s); in step, without the half step between them, 486 us.  4096 x 4096 x
 // 4096, one tile a CU, takes 60 us = 2.29 PFLOP/s: a tile's first copies and its result, 5 us, stand alone there.
 // PARTS: the workgroup sums a range of the contraction, where tiles are fewer than CUs and the contraction is long.
+// GATED: the sums of the contraction's first half wait in registers while the second half is summed, then SiLU(first) second is
+// the result: 4096 x (512 + 512) x 14336 into 8 bits 107 us, where two products into bf16 and the gated quantiser took 133 (in a graph;
+// 117 MB each that are not written and read).  The 256 x 256 tile has no registers for two sums, the smaller ones of
+// k_mm_ring not the 128 columns of a scale.
 template <int MT, int NT, int WM, int WN>
 struct MmTile {
   static constexpr int TM = 16 * MT * WM, TN = 16 * NT * WN, WAVES = WM * WN, HALF = WAVES / 2;
@@ -299,7 +317,7 @@ struct MmTile {
   static_assert(WAVES * MmResult<MT, NT>::BYTES <= LDS, "the result passes through the same memory");
 };
 
-template <int MT, int NT, int WM, int WN, bool PARTS>
+template <int MT, int NT, int WM, int WN, bool PARTS, bool GATED>
 __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_mm_tile(MmP p) {
   using T = MmTile<MT, NT, WM, WN>;
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
@@ -378,7 +396,7 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2,
   // The product of tile q of a step (row q / NT, column q % NT) is scaled and added LAG products later, when it is there; the
   // last ones of a step under the next step's first.
   constexpr int LAG = 3, Q = MT * NT;
-  f32x4 acc[NT][MT] = {}, d[LAG + 1] = {};
+  f32x4 acc[NT][MT] = {}, d[LAG + 1] = {}, gate[GATED ? NT : 1][GATED ? MT : 1];
   float s_last = 0.f;
   auto add = [&](int q, float s) {
 #pragma unroll
@@ -409,7 +427,8 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2,
     lds_barrier();
   }
   int wu = 0;          // unit of the step's rows of W
-  for (int t = 0; t < steps; ++t) {
+  auto run = [&](int t, int end) {
+  for (; t < end; ++t) {
     const int at_a = t % 2 * T::A_UNIT, at_w = T::W_AT + wu * T::W_UNIT;
     // this wave's copies of the step's A have landed, its LDS accesses are done
     wait_copies<T::CW>(t + 1, steps);
@@ -447,11 +466,29 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2,
     s_last = s[MT - 1];
     wu = wu < 2 ? wu + 1 : 0;
   }
-  if (half == 0) lds_barrier();    // as many as the other half
+  };
+  auto flush = [&] {
 #pragma unroll
-  for (int q = Q - LAG; q < Q; ++q) add(q, s_last);
-
+    for (int q = Q - LAG; q < Q; ++q) add(q, s_last);
+  };
+  if constexpr (GATED) {
+    for (int part = 0; part < 2; ++part) {
+      run(part * (steps / 2), (part + 1) * (steps / 2));
+      flush();
+      if (part) break;
+      s_last = 0.f;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) gate[j][i] = acc[j][i], acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  } else {
+    run(0, steps);
+    flush();
+  }
+  if (half == 0) lds_barrier();    // as many as the other half
   lds_barrier();      // everyone has read the last step
+  if constexpr (GATED) gate_sums<MT, NT>(acc, gate);
   mm_result<MT, NT, PARTS>(p, acc, z, m0 + arow, n0 + wrow, wave, lds);
 }
 
@@ -483,7 +520,7 @@ struct MmRing {
   static_assert(4 * MmResult<MT, NT>::BYTES <= LDS && TM <= 64 && TN <= SCALE_BLOCK, "one load of scales");
 };
 
-template <int MT, int NT>
+template <int MT, int NT, bool GATED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_mm_ring(MmP p) {
   using T = MmRing<MT, NT>;
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
@@ -592,10 +629,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   __builtin_amdgcn_s_waitcnt(0xC07F);
   lds_barrier();
   read(even, 0);
+  f32x4 gate[GATED ? NT : 1][GATED ? MT : 1];
+  auto turn = [&](int done) {
+    if constexpr (GATED) {
+      if (done != steps / 2) return;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) gate[j][i] = acc[j][i], acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
   for (int t = 0; t < steps; t += 2) {
     step(t, even, odd);
+    turn(t + 1);
     if (t + 1 < steps) step(t + 1, odd, even);
+    turn(t + 2);
   }
+  if constexpr (GATED) gate_sums<MT, NT>(acc, gate);
   __builtin_amdgcn_s_waitcnt(0xC07F);
   lds_barrier();      // everyone has read the last step
   mm_result<MT, NT, true>(p, acc, z, m0 + arow, n0 + wrow, wave, lds);
@@ -671,18 +721,20 @@ struct MmPlan {
   double est_us;
 };
 
-static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, MmPlan* best) {
+static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, int gated, MmPlan* best) {
   if (M < 0 || N <= 0 || K <= 0) return SVDMLP_INVALID_ARGUMENT;
   if (out_type != SVDMLP_F8 && out_type != SVDMLP_BF16) return SVDMLP_INVALID_ARGUMENT;
+  if (gated != 0 && (gated != 1 || K % (2 * SCALE_BLOCK))) return SVDMLP_INVALID_ARGUMENT;
   if (M >= int64_t(1) << 24 || N > int64_t(1) << 22 || K > int64_t(1) << 22) return SVDMLP_UNSUPPORTED;
   const int KB = (int)scale_blocks(K);
   best->kind = -1;
   for (int k = 0; k < MM_KINDS; ++k) {
     const MmKind& kind = MM_KIND[k];
     if (kind.max_rows && M > kind.max_rows) continue;
+    if (gated && k != MM_RING_64_128 && k != MM_TILE_128_256) continue;      // 128 columns in a workgroup, registers for two sums
     const int64_t tiles = ((M + kind.rows - 1) / kind.rows) * ((N + kind.cols - 1) / kind.cols);
     const bool large = k >= MM_TILE_128_256;
-    for (int r = 1; r <= (large ? 8 : 32) && r <= KB; r += !large ? r : r < 4 ? 1 : 2) {
+    for (int r = 1; r <= (gated ? 1 : large ? 8 : 32) && r <= KB; r += !large ? r : r < 4 ? 1 : 2) {
       MmPlan q;
       q.kind = k;
       q.tiles = tiles;
@@ -734,10 +786,10 @@ static void launch_join(const MmP& p, hipStream_t st) {
 
 template <int MT>
 static void launch_tile(const MmP& p, unsigned wgs, hipStream_t st) {
-  if (p.part) k_mm_tile<MT, 4, 2, 4, true><<<wgs, 512, 0, st>>>(p);
-  else k_mm_tile<MT, 4, 2, 4, false><<<wgs, 512, 0, st>>>(p);
+  if (p.part) k_mm_tile<MT, 4, 2, 4, true, false><<<wgs, 512, 0, st>>>(p);
+  else k_mm_tile<MT, 4, 2, 4, false, false><<<wgs, 512, 0, st>>>(p);
 }
-static void launch_mm(MmP& p, const MmPlan& q, hipStream_t st) {
+static void launch_mm(MmP& p, const MmPlan& q, bool gated, hipStream_t st) {
   const unsigned wgs = (unsigned)(q.tiles * q.ranges);
   const MmKind& kind = MM_KIND[q.kind];
   const int mtiles = (p.M + kind.rows - 1) / kind.rows, ntiles = (p.N + kind.cols - 1) / kind.cols;
@@ -745,10 +797,16 @@ static void launch_mm(MmP& p, const MmPlan& q, hipStream_t st) {
   p.band = q.kind >= MM_TILE_128_256 ? band_height(mtiles, wgs) : p.M > p.N ? ntiles : mtiles;
   switch (q.kind) {
     case MM_FEW: k_mm_few<<<wgs, 64 * FEW_WAVES, 0, st>>>(p); break;
-    case MM_RING_32: k_mm_ring<1, 2><<<wgs, 256, 0, st>>>(p); break;
-    case MM_RING_64: k_mm_ring<2, 2><<<wgs, 256, 0, st>>>(p); break;
-    case MM_RING_64_128: k_mm_ring<2, 4><<<wgs, 256, 0, st>>>(p); break;
-    case MM_TILE_128_256: launch_tile<4>(p, wgs, st); break;
+    case MM_RING_32: k_mm_ring<1, 2, false><<<wgs, 256, 0, st>>>(p); break;
+    case MM_RING_64: k_mm_ring<2, 2, false><<<wgs, 256, 0, st>>>(p); break;
+    case MM_RING_64_128:
+      if (gated) k_mm_ring<2, 4, true><<<wgs, 256, 0, st>>>(p);
+      else k_mm_ring<2, 4, false><<<wgs, 256, 0, st>>>(p);
+      break;
+    case MM_TILE_128_256:
+      if (gated) k_mm_tile<4, 4, 2, 4, false, true><<<wgs, 512, 0, st>>>(p);
+      else launch_tile<4>(p, wgs, st);
+      break;
     default: launch_tile<8>(p, wgs, st); break;
   }
 }
@@ -761,23 +819,23 @@ extern "C" {
 
 size_t svdmlp_scaled_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t out_type) {
   MmPlan q;
-  return plan_mm(M, N, K, out_type, &q) == SVDMLP_OK ? part_bytes(q, M, N) : 0;
+  return plan_mm(M, N, K, out_type, 0, &q) == SVDMLP_OK ? part_bytes(q, M, N) : 0;
 }
 
-int svdmlp_scaled_matmul_describe(int64_t M, int64_t N, int64_t K, int32_t out_type, char* buf, size_t buf_bytes) {
+int svdmlp_scaled_matmul_describe(int64_t M, int64_t N, int64_t K, int32_t out_type, int32_t gated, char* buf, size_t buf_bytes) {
   if (!buf || buf_bytes == 0) return SVDMLP_INVALID_ARGUMENT;
   buf[0] = 0;
   MmPlan q;
-  if (const int st = plan_mm(M, N, K, out_type, &q)) return st;
+  if (const int st = plan_mm(M, N, K, out_type, gated, &q)) return st;
   const int n = std::snprintf(buf, buf_bytes, "%s tiles=%lld ranges=%d est_us=%.1f]%s", MM_KIND[q.kind].name, (long long)q.tiles, q.ranges,
                               q.est_us, q.join ? " k_mm_join" : "");
   return n > 0 && (size_t)n < buf_bytes ? SVDMLP_OK : SVDMLP_INVALID_ARGUMENT;
 }
 
 int svdmlp_scaled_matmul(const svdmlp_scaled_matmul_args* a, void* hip_stream) {
-  if (!a || a->reserved != 0) return SVDMLP_INVALID_ARGUMENT;
+  if (!a) return SVDMLP_INVALID_ARGUMENT;
   MmPlan q;
-  if (const int st = plan_mm(a->M, a->N, a->K, a->out_type, &q)) return st;
+  if (const int st = plan_mm(a->M, a->N, a->K, a->out_type, a->gated, &q)) return st;
   if (const int st = check_codes(a->a, a->a_ld, a->K)) return st;
   if (const int st = check_codes(a->w, a->w_ld, a->K)) return st;
   if (!a->a_scales || !a->w_scales || !aligned_to(a->a_scales, 2) || !aligned_to(a->w_scales, 4) || a->a_scales_ld < a->M)
@@ -802,7 +860,7 @@ int svdmlp_scaled_matmul(const svdmlp_scaled_matmul_args* a, void* hip_stream) {
   p.out_type = a->out_type;
   p.ranges = q.ranges; p.range_blocks = q.range_blocks;
   hipStream_t st = (hipStream_t)hip_stream;
-  launch_mm(p, q, st);
+  launch_mm(p, q, a->gated != 0, st);
   if (q.join) launch_join(p, st);
   return launch_status();
 }

@@ -195,6 +195,7 @@ PyObject* scaled_matmul_args(Args v) {
   const int64_t device = integer(v[0]);
   svdmlp_scaled_matmul_args a = {};
   const int64_t M = a.M = integer(v[1]), N = a.N = integer(v[2]), K = a.K = integer(v[3]);
+  a.gated = small(v[11], "gated");
   const Matrix ca = codes(v[4], "a", M, K, device), sa = scales(v[5], "a", M, K, device), cw = codes(v[6], "w", N, K, device);
   a.a = ca.ptr, a.a_ld = ca.ld, a.a_scales = sa.ptr, a.a_scales_ld = sa.ld, a.w = cw.ptr, a.w_ld = cw.ld;
   a.w_scales = weight_scales(v[7], "w", N, K, device);
@@ -235,8 +236,8 @@ PyMethodDef methods[] = {
     {"norm_args", (PyCFunction)(void (*)())entry<norm_args, 20>, METH_FASTCALL,
      "(device, branch, residual, weight, bias, kind, eps, weight_plus, residual_scale, branch_scale, gate, gate_rows, gate_act, "
      "next_weight, next_bias, next_kind, next_eps, h, out, out_scales) -> svdmlp_norm_args"},
-    {"scaled_matmul_args", (PyCFunction)(void (*)())entry<scaled_matmul_args, 11>, METH_FASTCALL,
-     "(device, M, N, K, a, a_scales, w, w_scales, out, out_scales, workspace) -> svdmlp_scaled_matmul_args"},
+    {"scaled_matmul_args", (PyCFunction)(void (*)())entry<scaled_matmul_args, 12>, METH_FASTCALL,
+     "(device, M, N, K, a, a_scales, w, w_scales, out, out_scales, workspace, gated) -> svdmlp_scaled_matmul_args"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

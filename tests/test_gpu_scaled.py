@@ -157,6 +157,43 @@ def test_scaled_matmul(M, N, K, out):
         assert torch.equal(buf, before)
 
 
+GATED = [(1, 1, 256), (1, 1400, 512), (5, 130, 256), (16, 512, 1024), (64, 128, 768), (65, 129, 2048), (130, 385, 512), (300, 2600, 512),
+         (700, 1100, 1280), (1030, 2000, 256), (2100, 3585, 768), (1999, 4097, 512)]
+
+
+@pytest.mark.parametrize("out", [BF16, F8], ids=["bf16", "f8"])
+@pytest.mark.parametrize("M,N,K", GATED)
+def test_gated_product(M, N, K, out):
+    """SiLU(G) P of the two halves of the contraction.  G and P are known up to product_error; SiLU's slope is at most 1.1, and its
+    own error in fp32 that of an exponential whose argument is rounded (|g| EPS) and a few roundings."""
+    r = rng(11, M, N, K)
+    A, a = random_scaled(r, M, K, 16)
+    W, w = random_scaled(r, N, K, 32, True)
+    A.scales.mul_(1 / 16)         # gates of ordinary size and large ones
+    a = a / 16
+    half = K // 2
+    g, p = a[:, :half] @ w[:, :half].T, a[:, half:] @ w[:, half:].T
+    dg, dp = product_error(a[:, :half], w[:, :half]), product_error(a[:, half:], w[:, half:])
+    with np.errstate(over="ignore"):
+        s = ref.silu(g)
+    ds = 1.1 * dg + np.abs(s) * (np.abs(g) + dg + 8) * EPS
+    want, err = s * p, ds * np.abs(p) + np.abs(s) * dp + ds * dp + np.abs(s * p) * 2 * EPS
+    if out is F8:
+        q, buf = code_buffer(M, N, 16)
+        sc, sbuf = padded(-(-N // 128), M, BF16, 5, -7.0)
+        before, sbefore = buf.view(torch.uint8).clone(), sbuf.clone()
+        check_scaled(B.scaled_matmul(A, W, gated=True, out=(q, sc)), want, err)
+        q.view(torch.uint8).fill_(0x7F)
+        sc.fill_(-7.0)
+        assert torch.equal(buf.view(torch.uint8), before) and torch.equal(sbuf, sbefore)
+    else:
+        c, buf = padded(M, N, out, 3, -7.0, offset=1)
+        before = buf.clone()
+        check_float(B.scaled_matmul(A, W, gated=True, out=c), want, err)
+        c.fill_(-7.0)
+        assert torch.equal(buf, before)
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (16, 512, 14336), (128, 2048, 2048), (300, 1000, 270), (700, 1100, 2688)])
 def test_scaled_matmul_gives_the_same_bits_again(M, N, K):
     r = rng(2, M, N, K)

@@ -22,7 +22,7 @@ NORM = dict(rows=0, d=256, type=BF16, stream_type=BF16, out_type=F8, kind=B.NORM
             eps=1e-6, next_eps=1e-6, weight_plus=0.0, residual_scale=1.0, residual=0x1000, branch=0x2000, residual_ld=256,
             branch_ld=256, weight=0x3000, bias=0x3000, branch_scale=0x3000, gate=0x4000, gate_ld=256, next_weight=0x3000,
             next_bias=0x3000, h=0x5000, h_ld=256, out=0x6000, out_ld=256, out_scales=0x7000, out_scales_ld=64)
-MATMUL = dict(M=0, N=64, K=256, out_type=F8, reserved=0, a=0x1000, a_scales=0x2000, a_ld=256, a_scales_ld=64, w=0x3000, w_scales=0x4000,
+MATMUL = dict(M=0, N=64, K=256, out_type=F8, gated=0, a=0x1000, a_scales=0x2000, a_ld=256, a_scales_ld=64, w=0x3000, w_scales=0x4000,
               w_ld=256, c=0x5000, c_scales=0x6000, c_ld=64, c_scales_ld=64, workspace=0x7000, workspace_bytes=1 << 30)
 CALLS = {"svdmlp_quantize": (QUANTIZE, struct.Struct("=qqiiQQqqQQqq")),
          "svdmlp_norm": (NORM, struct.Struct("=qqiiiiiiqffffQQqqQQQQqQQQqQqQq")),
@@ -96,7 +96,9 @@ def test_norm_refuses(changed, want):
 
 
 @pytest.mark.parametrize("changed,want", [
-    (dict(M=-1), BAD), (dict(N=0), BAD), (dict(K=0), BAD), (dict(out_type=3), BAD), (dict(out_type=F32), BAD), (dict(reserved=1), BAD), (dict(a=0), BAD),
+    (dict(M=-1), BAD), (dict(N=0), BAD), (dict(K=0), BAD), (dict(out_type=3), BAD), (dict(out_type=F32), BAD), (dict(gated=2), BAD), (dict(gated=-1), BAD),
+    (dict(gated=1), OK), (dict(gated=1, K=128), BAD), (dict(gated=1, K=384, a_ld=384, w_ld=384), BAD), (dict(gated=1, out_type=BF16), OK),
+    (dict(a=0), BAD),
     (dict(a=0x1008), BAD), (dict(a_ld=248), BAD), (dict(a_ld=240), BAD), (dict(w=0), BAD), (dict(w=0x3001), BAD), (dict(w_ld=255), BAD),
     (dict(a_scales=0), BAD), (dict(w_scales=0), BAD), (dict(a_scales=0x2001), BAD), (dict(M=65), BAD), (dict(c=0), BAD), (dict(c=0x5004), BAD),
     (dict(c_ld=56), BAD), (dict(c_scales=0), BAD), (dict(c=0x1000), BAD), (dict(c=0x3000), BAD), (dict(out_type=BF16, c=0x5001), BAD),
@@ -145,6 +147,18 @@ def test_the_gpu_tests_sizes_reach_every_kernel_of_the_product():
 ])
 def test_the_products_planner_takes_what_measured_fastest(M, N, K, kernel):
     assert B.svdmlp_scaled_matmul_describe(M, N, K, BF16).startswith("k_mm_" + kernel)
+
+
+def test_gated_products_have_two_kernels():
+    """Sizes of the GPU tests reach both; none cuts the contraction."""
+    from tests.test_gpu_scaled import GATED
+    seen = {B.svdmlp_scaled_matmul_describe(M, N, K, F8, True).split(" ")[0] for M, N, K in GATED}
+    assert seen == {"k_mm_ring[tile=64x128", "k_mm_tile[tile=128x256"}
+    for M, N, K in GATED:
+        assert "ranges=1 " in B.svdmlp_scaled_matmul_describe(M, N, K, F8, True)
+    for K in (16, 128, 384):
+        with pytest.raises(B.SvdMlpError):
+            B.svdmlp_scaled_matmul_describe(64, 64, K, F8, True)
 
 
 class _OnDevice(torch.Tensor):
@@ -243,7 +257,7 @@ def test_what_the_binding_hands_over(monkeypatch):
 
     (a, sa), o = f8(5, 300, 36, 1), strided(5, 70, bf, 9)
     w = B.Scaled(strided(70, 300, torch.float8_e4m3fn, 4), torch.zeros(1, 3))
-    mm = dict(M=5, N=70, K=300, out_type=BF16, reserved=0, a=a.data_ptr(), a_scales=sa.data_ptr(), a_ld=336, a_scales_ld=6,
+    mm = dict(M=5, N=70, K=300, out_type=BF16, gated=0, a=a.data_ptr(), a_scales=sa.data_ptr(), a_ld=336, a_scales_ld=6,
               w=w.codes.data_ptr(), w_scales=w.scales.data_ptr(), w_ld=304, c=o.data_ptr(), c_scales=0, c_ld=79, c_scales_ld=0,
               workspace=0, workspace_bytes=B.svdmlp_scaled_matmul_workspace_bytes(5, 70, 300, BF16))
     got = fields_of(monkeypatch, lambda: B.scaled_matmul((a, sa), w, out=o))
@@ -252,6 +266,9 @@ def test_what_the_binding_hands_over(monkeypatch):
     got = fields_of(monkeypatch, lambda: B.scaled_matmul((a, sa), w, out=(q, sq)))
     assert {**got, "workspace": 0} == {**mm, "out_type": F8, "c": q.data_ptr(), "c_ld": 80, "c_scales": sq.data_ptr(), "c_scales_ld": 5,
                                        "workspace_bytes": B.svdmlp_scaled_matmul_workspace_bytes(5, 70, 300, F8)}
+    g8, gw = f8(5, 512, 0, 0), B.empty_scaled(70, 512, "cpu", 128)
+    got = fields_of(monkeypatch, lambda: B.scaled_matmul(g8, gw, gated=True))
+    assert (got["gated"], got["out_type"], got["K"], got["workspace"], got["workspace_bytes"]) == (1, BF16, 512, 0, 0)
     a8, w8 = f8(16, 14336, 0, 0), B.empty_scaled(512, 14336, "cpu", 128)
     got = fields_of(monkeypatch, lambda: B.scaled_matmul(a8, w8, out_dtype=torch.float8_e4m3fn))
     assert got["workspace"] and got["workspace_bytes"] == B.svdmlp_scaled_matmul_workspace_bytes(16, 512, 14336, F8) > 0
