@@ -305,8 +305,8 @@ __device__ __forceinline__ void wait_copies(int t, int steps) {
 // 4096, one tile a CU, takes 60 us = 2.29 PFLOP/s: a tile's first copies and its result, 5 us, stand alone there.
 // PARTS: the workgroup sums a range of the contraction, where tiles are fewer than CUs and the contraction is long.
 // GATED: the sums of the contraction's first half wait in registers while the second half is summed, then SiLU(first) second is
-// the result: 4096 x (512 + 512) x 14336 into 8 bits 107 us, where two products into bf16 and the gated quantiser took 133 (in a graph;
-// 117 MB each that are not written and read).  The 256 x 256 tile has no registers for two sums, the smaller ones of
+// the result: 4096 x (512 + 512) x 14336 into 8 bits 96-107 us, where two products into bf16 and the gated quantiser took 133 (in a
+// graph; 117 MB each that are not written and read).  The 256 x 256 tile has no registers for two sums, the smaller ones of
 // k_mm_ring not the 128 columns of a scale.
 template <int MT, int NT, int WM, int WN>
 struct MmTile {
@@ -696,8 +696,10 @@ __global__ __launch_bounds__(256) void k_mm_join(MmP p) {
 //   4096 x 8192 x 16384 tile 256x256 434 / 446, tile 128x256 540 / 560
 //   286 x 13184 x 7424  tile 256x256 in 4 ranges 62 / 58, in one 148 / 143
 //   4096 x 14336 x 512  ring 64x64 45 / 50, tile 128x256 in 4 ranges 50 / 44, in one 105 / 93
-// (Further tiles measured and not kept: 128 x 128 with four waves, 256 x 128, 128 x 64, 32 x 128: level or behind one of these.)
-enum { MM_FEW = 0, MM_RING_32, MM_RING_64, MM_RING_64_128, MM_TILE_128_256, MM_TILE_256, MM_KINDS };
+// Gated, into 8 bits: 1 x 1024 x 14336  ring 32x128 7.3 / 7.4, ring 64x128 9.4 / 9.6;  512 x 1024 x 14336  tile 128x256 15.5 / 16.4, ring
+// 64x128 26 / 22;  4096 x 1024 x 14336  tile 128x256 93 / 96, ring 64x128 167 / 129.
+// (Further tiles measured and not kept: 128 x 128 with four waves, 256 x 128, 128 x 64: level or behind one of these.)
+enum { MM_FEW = 0, MM_RING_32, MM_RING_64, MM_RING_64_128, MM_TILE_128_256, MM_TILE_256, MM_RING_32_128, MM_KINDS };
 struct MmKind {
   const char* name;
   int rows, cols, max_rows;      // of a tile; rows of A that it takes (0: any)
@@ -710,6 +712,7 @@ constexpr MmKind MM_KIND[MM_KINDS] = {
     {"k_mm_ring[tile=64x128", 64, 128, 0, 0.485, 0.577, 0.393, 0.98},
     {"k_mm_tile[tile=128x256", 128, 256, 0, 1.02, 1.9, 1.0, 3.25},
     {"k_mm_tile[tile=256x256", 256, 256, 0, 1.43, 3.1, 1.6, 5.4},
+    {"k_mm_ring[tile=32x128", 32, 128, 0, 0.45, 0.57, 0.255, 0.8},     // gated only: level with the others or behind them elsewhere
 };
 constexpr double LAUNCH_US = 2.5, JOIN_US = 2.6, JOIN_RANGE_US = 0.1, HBM_BYTES_PER_US = 7.05e6, PART_BYTES_PER_US = 5.2e6;
 constexpr int MM_CUS = 256;      // the model's device, so that a result's order of sums goes by the extents alone
@@ -731,9 +734,9 @@ static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, int gated, MmP
   for (int k = 0; k < MM_KINDS; ++k) {
     const MmKind& kind = MM_KIND[k];
     if (kind.max_rows && M > kind.max_rows) continue;
-    if (gated && k != MM_RING_64_128 && k != MM_TILE_128_256) continue;      // 128 columns in a workgroup, registers for two sums
+    if (k == MM_RING_32_128 ? !gated : gated && k != MM_RING_64_128 && k != MM_TILE_128_256) continue;      // 128 columns in a workgroup, registers for two sums
     const int64_t tiles = ((M + kind.rows - 1) / kind.rows) * ((N + kind.cols - 1) / kind.cols);
-    const bool large = k >= MM_TILE_128_256;
+    const bool large = k == MM_TILE_128_256 || k == MM_TILE_256;
     for (int r = 1; r <= (gated ? 1 : large ? 8 : 32) && r <= KB; r += !large ? r : r < 4 ? 1 : 2) {
       MmPlan q;
       q.kind = k;
@@ -753,11 +756,12 @@ static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, int gated, MmP
         steps = (steps + FEW_WAVES - 1) / FEW_WAVES * FEW_WAVES;
         step += 0.0205 / FEW_WAVES * M * per_cu;
       }
+      if (gated && k == MM_RING_64_128) step *= 1.4;     // registers for two sums: fewer waves
       if (!on_lines) {
         step *= k == MM_TILE_256 ? 1.07 : 1.28;
         hbm *= 1.84;
       }
-      double t = kind.tile * per_cu + steps * step;
+      double t = kind.tile * (gated ? 1.5 : 1.) * per_cu + steps * step;      // SiLU of the tile
       if (t < hbm) t = hbm;
       q.est_us = LAUNCH_US + t + (q.join ? JOIN_US + JOIN_RANGE_US * r + 8. * M * N * r / PART_BYTES_PER_US : 0.);
       if (best->kind < 0 || q.est_us < best->est_us) *best = q;
@@ -794,7 +798,7 @@ static void launch_mm(MmP& p, const MmPlan& q, bool gated, hipStream_t st) {
   const MmKind& kind = MM_KIND[q.kind];
   const int mtiles = (p.M + kind.rows - 1) / kind.rows, ntiles = (p.N + kind.cols - 1) / kind.cols;
   p.tiles = (int)q.tiles;
-  p.band = q.kind >= MM_TILE_128_256 ? band_height(mtiles, wgs) : p.M > p.N ? ntiles : mtiles;
+  p.band = q.kind == MM_TILE_128_256 || q.kind == MM_TILE_256 ? band_height(mtiles, wgs) : p.M > p.N ? ntiles : mtiles;
   switch (q.kind) {
     case MM_FEW: k_mm_few<<<wgs, 64 * FEW_WAVES, 0, st>>>(p); break;
     case MM_RING_32: k_mm_ring<1, 2, false><<<wgs, 256, 0, st>>>(p); break;
@@ -807,6 +811,7 @@ static void launch_mm(MmP& p, const MmPlan& q, bool gated, hipStream_t st) {
       if (gated) k_mm_tile<4, 4, 2, 4, false, true><<<wgs, 512, 0, st>>>(p);
       else launch_tile<4>(p, wgs, st);
       break;
+    case MM_RING_32_128: k_mm_ring<1, 4, true><<<wgs, 256, 0, st>>>(p); break;
     default: launch_tile<8>(p, wgs, st); break;
   }
 }

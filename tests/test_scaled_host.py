@@ -149,11 +149,11 @@ def test_the_products_planner_takes_what_measured_fastest(M, N, K, kernel):
     assert B.svdmlp_scaled_matmul_describe(M, N, K, BF16).startswith("k_mm_" + kernel)
 
 
-def test_gated_products_have_two_kernels():
-    """Sizes of the GPU tests reach both; none cuts the contraction."""
+def test_gated_products_have_three_kernels():
+    """Sizes of the GPU tests reach all; none cuts the contraction."""
     from tests.test_gpu_scaled import GATED
     seen = {B.svdmlp_scaled_matmul_describe(M, N, K, F8, True).split(" ")[0] for M, N, K in GATED}
-    assert seen == {"k_mm_ring[tile=64x128", "k_mm_tile[tile=128x256"}
+    assert seen == {"k_mm_ring[tile=32x128", "k_mm_ring[tile=64x128", "k_mm_tile[tile=128x256"}
     for M, N, K in GATED:
         assert "ranges=1 " in B.svdmlp_scaled_matmul_describe(M, N, K, F8, True)
     for K in (16, 128, 384):
