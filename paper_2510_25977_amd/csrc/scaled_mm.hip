@@ -397,7 +397,7 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2,
   // last ones of a step under the next step's first.
   constexpr int LAG = 3, Q = MT * NT;
   f32x4 acc[NT][MT] = {}, d[LAG + 1] = {}, gate[GATED ? NT : 1][GATED ? MT : 1];
-  float s_last = 0.f;
+  float s_last = 0.f;     // (a product that is NaN stays NaN times zero: its element is NaN then already)
   auto add = [&](int q, float s) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[q % NT][q / NT][e] += d[q % (LAG + 1)][e] * s;
@@ -427,45 +427,46 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2,
     lds_barrier();
   }
   int wu = 0;          // unit of the step's rows of W
+  // steps t .. end - 1
   auto run = [&](int t, int end) {
-  for (; t < end; ++t) {
-    const int at_a = t % 2 * T::A_UNIT, at_w = T::W_AT + wu * T::W_UNIT;
-    // this wave's copies of the step's A have landed, its LDS accesses are done
-    wait_copies<T::CW>(t + 1, steps);
-    __builtin_amdgcn_s_waitcnt(0xC07F);
-    lds_barrier();
-    float s[MT];
+    for (; t < end; ++t) {
+      const int at_a = t % 2 * T::A_UNIT, at_w = T::W_AT + wu * T::W_UNIT;
+      // this wave's copies of the step's A have landed, its LDS accesses are done
+      wait_copies<T::CW>(t + 1, steps);
+      __builtin_amdgcn_s_waitcnt(0xC07F);
+      lds_barrier();
+      float s[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) s[i] = scale_next(i);
-    if (t + 1 < steps) load_scales(t + 1);
-    issue_a(aoff, t + 1, (t + 1) % 2);
-    issue_w(woff, t + 2, wu > 0 ? wu - 1 : 2);
-    i32x8 fw[NT], fa[2];
-    fa[0] = frag(at_a, arow);
+      for (int i = 0; i < MT; ++i) s[i] = scale_next(i);
+      if (t + 1 < steps) load_scales(t + 1);
+      issue_a(aoff, t + 1, (t + 1) % 2);
+      issue_w(woff, t + 2, wu > 0 ? wu - 1 : 2);
+      i32x8 fw[NT], fa[2];
+      fa[0] = frag(at_a, arow);
 #pragma unroll
-    for (int j = 0; j < NT; ++j) fw[j] = frag(at_w, wrow + 16 * j);
-    __builtin_amdgcn_sched_barrier(0);
+      for (int j = 0; j < NT; ++j) fw[j] = frag(at_w, wrow + 16 * j);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      if (i == MT / 2) {
-        wait_copies<T::CA + T::CW>(t + 2, steps);
-        lds_barrier();
+      for (int i = 0; i < MT; ++i) {
+        if (i == MT / 2) {
+          wait_copies<T::CA + T::CW>(t + 2, steps);
+          lds_barrier();
+        }
+        if (i + 1 < MT) fa[(i + 1) % 2] = frag(at_a, arow + 16 * (i + 1));
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          __builtin_amdgcn_sched_barrier(0);
+          const int q = i * NT + j;
+          d[q % (LAG + 1)] = mfma_f8(fw[j], fa[i % 2], f32x4{0.f, 0.f, 0.f, 0.f});
+          __builtin_amdgcn_sched_barrier(0);
+          if (q < LAG) add(Q + q - LAG, s_last);
+          else add(q - LAG, s[(q - LAG) / NT]);
+        }
       }
-      if (i + 1 < MT) fa[(i + 1) % 2] = frag(at_a, arow + 16 * (i + 1));
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        __builtin_amdgcn_sched_barrier(0);
-        const int q = i * NT + j;
-        d[q % (LAG + 1)] = mfma_f8(fw[j], fa[i % 2], f32x4{0.f, 0.f, 0.f, 0.f});
-        __builtin_amdgcn_sched_barrier(0);
-        if (q < LAG) add(Q + q - LAG, s_last);
-        else add(q - LAG, s[(q - LAG) / NT]);
-      }
+      __builtin_amdgcn_sched_barrier(0);
+      s_last = s[MT - 1];
+      wu = wu < 2 ? wu + 1 : 0;
     }
-    __builtin_amdgcn_sched_barrier(0);
-    s_last = s[MT - 1];
-    wu = wu < 2 ? wu + 1 : 0;
-  }
   };
   auto flush = [&] {
 #pragma unroll

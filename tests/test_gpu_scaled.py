@@ -194,6 +194,21 @@ def test_gated_product(M, N, K, out):
         assert torch.equal(buf, before)
 
 
+@pytest.mark.parametrize("M,N", [(40, 200), (300, 4000), (1500, 3600)])
+def test_gated_product_keeps_nan_to_its_row(M, N):
+    r = rng(12, M, N)
+    (A, _), (W, _) = random_scaled(r, M, 768, 0), random_scaled(r, N, 768, 0, True)
+    good = B.scaled_matmul(A, W, gated=True).float()
+    A.codes.view(torch.uint8)[7, 100] = 0x7F           # in a gate's operand
+    A.codes.view(torch.uint8)[M - 2, 700] = 0xFF       # in an up product's
+    got = B.scaled_matmul(A, W, gated=True).float()
+    bad = torch.isnan(got)
+    assert bad[7].all() and bad[M - 2].all() and int(bad.sum()) == 2 * N
+    bad[:] = False
+    bad[[7, M - 2]] = True
+    assert torch.equal(got[~bad], good[~bad]) and torch.isfinite(good).all()
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (16, 512, 14336), (128, 2048, 2048), (300, 1000, 270), (700, 1100, 2688)])
 def test_scaled_matmul_gives_the_same_bits_again(M, N, K):
     r = rng(2, M, N, K)
