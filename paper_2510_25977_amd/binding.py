@@ -569,6 +569,11 @@ class SvdMlpF8:
             self.first = weights(ranked(Ug), ranked(Uu))
             self.gate_up = quantize(torch.cat([rank_rows(Vg).t(), rank_rows(Vu).t()], 1), block_rows=SCALE_BLOCK)
             self.down, self.last = weights(ranked(Ud)), weights(rank_rows(Vd))
+        # A forward may run on another stream than this one, and nothing orders it after the quantiser: so, as SvdMlp's, its
+        # operands are there when it is.  (A stream that is being captured cannot be waited for: the graph quantises.)
+        with torch.cuda.device(Ug.device):
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream().synchronize()
 
     def out_features(self) -> int:
         return self.d if self.kind == SVDMLP_GATED else self.ffn

@@ -575,3 +575,43 @@ def test_a_block_on_a_side_stream_and_in_a_graph(M):
         eager = block(inputs[i], mlp, *w)
         torch.cuda.synchronize()
         assert same(captured, i) and same(eager, i), i
+
+
+def test_a_forward_on_a_side_stream_right_after_construction():
+    """The constructor has quantised the factors when it returns, however much its stream had to do before: a forward on another
+    stream, which nothing orders after it, gives the bits of one on the same."""
+    r = rng(13)
+    f = make_block(r, 512, 768, 128, 128)
+    x = torch.from_numpy(r.normal(size=(40, 512))).to(BF16).to(dev())
+    n = B.quantize(x)
+    busy = torch.randn(4096, 4096, device=dev())
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        busy = torch.mm(busy, busy).clamp_(-1, 1)
+    mlp = B.SvdMlpF8(**f)
+    y = mlp(n, stream=side)
+    side.synchronize()
+    want = mlp(n)
+    torch.cuda.synchronize()
+    assert torch.equal(y, want) and torch.isfinite(want).all()
+
+
+def test_a_block_made_in_a_graph():
+    """Its factors are quantised by the graph then, and again by each replay."""
+    r = rng(14)
+    f = make_block(r, 512, 768, 128, 128)
+    x = torch.from_numpy(r.normal(size=(40, 512))).to(BF16).to(dev())
+    want = B.SvdMlpF8(**f)(x)
+    f2 = make_block(r, 512, 768, 128, 128)
+    want2 = B.SvdMlpF8(**f2)(x)
+    own = {k: v.clone() for k, v in f.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = B.SvdMlpF8(**own)(x)
+    for factors, expected in ((f, want), (f2, want2), (f, want)):
+        for k, v in factors.items():
+            own[k].copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, expected)

@@ -366,6 +366,40 @@ def test_what_a_call_on_a_stream_makes_is_that_streams(monkeypatch):
             call(elsewhere)
 
 
+@pytest.mark.parametrize("kind,quantised", [(B.SVDMLP_GATED, 4), (B.SVDMLP_LINEAR, 2)])
+def test_a_block_is_quantised_when_its_constructor_returns(monkeypatch, kind, quantised):
+    """A forward may run on any stream: the constructor waits for its own, where the factors are quantised, after the last of
+    them and before a forward can be called.  While that stream is captured nothing runs that could be waited for."""
+    done, capturing = [], [False]
+
+    class on:
+        def __init__(self, where):
+            pass
+
+        def __enter__(self):
+            pass
+
+        def __exit__(self, *e):
+            pass
+
+    stream = types.SimpleNamespace(synchronize=lambda: done.append("synchronize"))
+    monkeypatch.setattr(torch.cuda, "device", on)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: stream)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    monkeypatch.setattr(B, "_run", lambda name, *a: done.append(name))
+    monkeypatch.setattr(B, "_device_of", lambda t, what: -1)       # what is made between the products lies on the CPU here
+    f = dict(Ug=fake(256, 64), Vg=fake(64, 512), Uu=fake(256, 64), Vu=fake(64, 512), Ud=fake(512, 40), Vd=fake(40, 256))
+    mlp = B.SvdMlpF8(kind=kind, **f)
+    assert done == ["svdmlp_quantize"] * quantised + ["synchronize"]
+    mlp.forward(fake(4, 256), stream=types.SimpleNamespace(device_index=-1))
+    assert done[quantised + 1:] == ["svdmlp_quantize"] + ["svdmlp_scaled_matmul"] * quantised      # as many products as operands
+    done.clear()
+    capturing[0] = True
+    B.SvdMlpF8(kind=kind, **f)
+    assert done == ["svdmlp_quantize"] * quantised
+
+
 def test_the_e4m3_table_of_the_oracle():
     codes = torch.arange(256, dtype=torch.int32).to(torch.uint8)
     want = codes.view(torch.float8_e4m3fn).double().numpy()
