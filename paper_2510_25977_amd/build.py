@@ -3,10 +3,12 @@
     python -m paper_2510_25977_amd.build [--force]
 
 Both are built next to this file, as ``libsvdmlp.so`` and ``_tensors.so``, so that they travel with the source
-tree; tests, ``bench.py`` and ``__graft_entry__.smoke()`` load these files and never compile.
+tree; tests, ``bench.py`` and ``__graft_entry__.smoke()`` load these files and never compile.  The library needs hipcc alone;
+``_tensors.so`` needs torch and a host compiler, and is left out, with a message, where there is no torch.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import re
 import subprocess
@@ -95,11 +97,13 @@ def build_tensors() -> None:
 
 
 def build(force: bool = True, verbose: bool = False) -> Path:
-    """Compile every HIP source and link ``libsvdmlp.so``, and compile ``_tensors.so``.  Always recompiles unless force=False
-    and both are newer than every source."""
+    """Compile every HIP source and link ``libsvdmlp.so``, and compile ``_tensors.so`` where there is torch.  Always recompiles
+    unless force=False and both are newer than every source.  The library is linked whatever comes of ``_tensors.so``."""
     srcs = sources()
     deps = srcs + sorted(CSRC.glob("*.h")) + [CSRC / "tensors.cpp", HERE.parent / "include" / "svdmlp.h"]
-    if not force and all(lib.exists() and all(lib.stat().st_mtime >= s.stat().st_mtime for s in deps) for lib in (LIB, TENSORS)):
+    with_tensors = importlib.util.find_spec("torch") is not None
+    libs = (LIB, TENSORS) if with_tensors else (LIB,)
+    if not force and all(lib.exists() and all(lib.stat().st_mtime >= s.stat().st_mtime for s in deps) for lib in libs):
         return LIB
     OBJDIR.mkdir(exist_ok=True)
 
@@ -126,17 +130,20 @@ def build(force: bool = True, verbose: bool = False) -> Path:
     # sources with hand-written memory instructions that take an SGPR base: their generated assembly is checked
     asm_srcs = [s for s in srcs if re.search(r'asm volatile\("[^;]*global_(load|store)', s.read_text())]
     with ThreadPoolExecutor(max_workers=min(8, len(srcs) + len(asm_srcs) + 1)) as ex:
-        tensors = ex.submit(build_tensors)
+        tensors = ex.submit(build_tensors) if with_tensors else None
         hz = [ex.submit(hazards_of, s) for s in asm_srcs]
         objs = list(ex.map(compile_one, srcs))
         hazards = [f for h in hz for f in h.result()]
-        tensors.result()
     if hazards:
         raise RuntimeError("SGPR-to-memory-address hazard inside inline asm (see check_sgpr_hazards):\n" + "\n".join(hazards))
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", str(LIB), *map(str, objs)]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("link failed:\n" + res.stdout + res.stderr)
+    if tensors is None:
+        print(f"no torch: {TENSORS.name}, which the operators of the binding need, is not built", file=sys.stderr)
+    else:
+        tensors.result()
     return LIB
 
 
