@@ -376,12 +376,17 @@ _checks = None
 
 
 def _tensors():
-    """The extension module that checks tensors and packs arguments (raises if it has not been built)."""
+    """The extension module that checks tensors and packs arguments (raises if it has not been built, or not for this torch)."""
     global _checks
     if _checks is None:
+        how = "build it with `python -m paper_2510_25977_amd.build`"
         if not TENSORS_PATH.exists():
-            raise FileNotFoundError(f"{TENSORS_PATH} not found: build it with `python -m paper_2510_25977_amd.build`")
-        from . import _tensors as _checks
+            raise FileNotFoundError(f"{TENSORS_PATH} not found: {how}")
+        from . import _tensors
+        from .build import tensors_for
+        if _tensors.built_for != tensors_for():
+            raise ImportError(f"{TENSORS_PATH} is built for {_tensors.built_for}, this is {tensors_for()}: {how}")
+        _checks = _tensors
     return _checks
 
 

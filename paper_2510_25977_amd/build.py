@@ -81,29 +81,38 @@ def check_sgpr_hazards(asm: str) -> list:
     return found
 
 
+def tensors_for() -> str:
+    """What ``_tensors.so`` has to be compiled for: it reads structures of the running Python and torch."""
+    import torch
+    return f"{sys.implementation.cache_tag}, torch {torch.__version__}"
+
+
 def build_tensors() -> None:
-    """Compile the extension module of the binding against the installed torch."""
+    """Compile the extension module of the binding against the installed torch, and note which that was."""
     import sysconfig
     import torch
     from torch.utils.cpp_extension import include_paths
     includes = [f"-I{p}" for p in [*include_paths(), sysconfig.get_path("include")]]
     libs = Path(torch.__file__).resolve().parent / "lib"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *includes, str(CSRC / "tensors.cpp"), "-o", str(TENSORS),
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DBUILT_FOR="{tensors_for()}"', *includes, str(CSRC / "tensors.cpp"), "-o", str(TENSORS),
            f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("the C++ compiler failed on tensors.cpp:\n" + (res.stdout + res.stderr)[-4000:])
+    (OBJDIR / "tensors.txt").write_text(tensors_for())
 
 
 def build(force: bool = True, verbose: bool = False) -> Path:
     """Compile every HIP source and link ``libsvdmlp.so``, and compile ``_tensors.so`` where there is torch.  Always recompiles
-    unless force=False and both are newer than every source.  The library is linked whatever comes of ``_tensors.so``."""
+    unless force=False, both are newer than every source and ``_tensors.so`` is for this torch.  The library is linked whatever comes of ``_tensors.so``."""
     srcs = sources()
     deps = srcs + sorted(CSRC.glob("*.h")) + [CSRC / "tensors.cpp", HERE.parent / "include" / "svdmlp.h"]
     with_tensors = importlib.util.find_spec("torch") is not None
     libs = (LIB, TENSORS) if with_tensors else (LIB,)
-    if not force and all(lib.exists() and all(lib.stat().st_mtime >= s.stat().st_mtime for s in deps) for lib in libs):
+    noted = OBJDIR / "tensors.txt"
+    if (not force and all(lib.exists() and all(lib.stat().st_mtime >= s.stat().st_mtime for s in deps) for lib in libs)
+            and (not with_tensors or (noted.exists() and noted.read_text() == tensors_for()))):
         return LIB
     OBJDIR.mkdir(exist_ok=True)
 

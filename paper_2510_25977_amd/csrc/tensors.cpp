@@ -243,4 +243,12 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__tensors() { return PyModule_Create(&module_def); }
+// built_for: the Python and torch that this was compiled for, which the binding compares with those it runs on
+PyMODINIT_FUNC PyInit__tensors() {
+  PyObject* m = PyModule_Create(&module_def);
+  if (m && PyModule_AddStringConstant(m, "built_for", BUILT_FOR) < 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}

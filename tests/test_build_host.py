@@ -60,3 +60,18 @@ def test_a_source_that_does_not_compile_stops_the_build(compiler):
     with pytest.raises(RuntimeError, match="norm.hip"):
         bld.build(force=True)
     assert not bld.LIB.exists()
+
+
+def test_the_tensor_checks_are_rebuilt_for_another_torch(compiler, monkeypatch):
+    """They are compiled against one torch and one Python: under another one they are not current, however new."""
+    import torch
+    bld.build(force=True)
+    compiler.made.clear()
+    bld.build(force=False)
+    assert not compiler.made
+    monkeypatch.setattr(torch, "__version__", "0.0.0")
+    bld.build(force=False)
+    assert "_tensors.so" in compiler.made
+    compiler.made.clear()
+    bld.build(force=False)
+    assert not compiler.made

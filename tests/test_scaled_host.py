@@ -303,6 +303,15 @@ def test_a_missing_build_is_an_error(monkeypatch, tmp_path):
         B.quantize(fake(4, 256), out=B.empty_scaled(4, 256, "cpu"))
 
 
+def test_a_build_for_another_torch_is_an_error(monkeypatch):
+    """The tensor checks read torch's own structures, so those compiled for another version are refused and not called."""
+    monkeypatch.setattr(B, "_checks", None)
+    monkeypatch.setattr(torch, "__version__", "0.0.0")
+    for _ in range(2):
+        with pytest.raises(ImportError, match="0.0.0"):
+            B.quantize(fake(4, 256), out=B.empty_scaled(4, 256, "cpu"))
+
+
 def test_a_call_on_another_device_makes_it_current(monkeypatch):
     """Kernels go to the current device, so an operator whose tensors lie elsewhere switches to theirs and back, and asks for
     the current stream of that device."""
