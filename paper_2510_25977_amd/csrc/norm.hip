@@ -175,14 +175,14 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
 }
 
 template <class T, class S, int TPR, int NV, RowEnd END>
-static void run_norm(const NormP& p, hipStream_t st) {
+static hipError_t run_norm(const NormP& p, hipStream_t st) {
   constexpr int per = TPR == 64 ? 4 : 1;
-  k_norm<T, S, TPR, NV, END><<<(unsigned)((p.rows + per - 1) / per), TPR * per, 0, st>>>(p);
+  return launch(k_norm<T, S, TPR, NV, END>, (unsigned)((p.rows + per - 1) / per), TPR * per, p, st);
 }
 template <class T, class S, int TPR, int NV>
-static void run_norm(const NormP& p, hipStream_t st) {
-  if (p.d % 8 == 0) run_norm<T, S, TPR, NV, WHOLE>(p, st);
-  else run_norm<T, S, TPR, NV, OVERLAP>(p, st);
+static hipError_t run_norm(const NormP& p, hipStream_t st) {
+  if (p.d % 8 == 0) return run_norm<T, S, TPR, NV, WHOLE>(p, st);
+  return run_norm<T, S, TPR, NV, OVERLAP>(p, st);
 }
 
 // As few vectors a thread as a workgroup's size allows: a row's chain (loads, sums over the workgroup, stores) is what a CU has
@@ -192,7 +192,7 @@ static void run_norm(const NormP& p, hipStream_t st) {
 static int row_threads(int64_t d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 16384 ? 512 : 1024; }
 
 template <class T, class S>
-static void launch_norm(const NormP& p, hipStream_t st) {
+static hipError_t launch_norm(const NormP& p, hipStream_t st) {
   if (row_end(p.d) == SHORT) return run_norm<T, S, 64, 1, SHORT>(p, st);
   switch (row_threads(p.d)) {
     case 64: return run_norm<T, S, 64, 1>(p, st);
@@ -201,9 +201,9 @@ static void launch_norm(const NormP& p, hipStream_t st) {
     case 512: break;
     default: return run_norm<T, S, 1024, 4>(p, st);
   }
-  if (p.d <= 4096) run_norm<T, S, 512, 1>(p, st);
-  else if (p.d <= 8192) run_norm<T, S, 512, 2>(p, st);
-  else run_norm<T, S, 512, 4>(p, st);
+  if (p.d <= 4096) return run_norm<T, S, 512, 1>(p, st);
+  if (p.d <= 8192) return run_norm<T, S, 512, 2>(p, st);
+  return run_norm<T, S, 512, 4>(p, st);
 }
 
 static bool known_norm(int k) { return k == SVDMLP_NORM_NONE || k == SVDMLP_NORM_RMS || k == SVDMLP_NORM_LAYER; }
@@ -252,8 +252,7 @@ extern "C" int svdmlp_norm(const svdmlp_norm_args* a, void* hip_stream) {
   p.eps = a->eps; p.next_eps = a->next_eps; p.weight_plus = a->weight_plus; p.residual_scale = a->residual_scale;
   p.inv_d = (float)(1.0 / (double)a->d);
   hipStream_t st = (hipStream_t)hip_stream;
-  if (a->type == SVDMLP_F32) launch_norm<float, float>(p, st);
-  else if (a->stream_type == SVDMLP_F32) launch_norm<__bf16, float>(p, st);
-  else launch_norm<__bf16, __bf16>(p, st);
-  return launch_status();
+  if (a->type == SVDMLP_F32) return status_of(launch_norm<float, float>(p, st));
+  if (a->stream_type == SVDMLP_F32) return status_of(launch_norm<__bf16, float>(p, st));
+  return status_of(launch_norm<__bf16, __bf16>(p, st));
 }

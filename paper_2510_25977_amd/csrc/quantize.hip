@@ -87,23 +87,23 @@ __global__ __launch_bounds__(256) void k_quantize_block(QuantP p) {
 // 1 / 2 / 4 blocks a group take, in a graph, 66.8 / 63.6 / 59.0 us at 4096 x 14336 gated, 6.0 / 5.6 / 5.2 us at 16 x 14336; with
 // four, 1777 x 7301 gated takes 15.1 us (4.3 TB/s), 1777 x 7304 14.4.  Rows of less than eight columns have one block.
 template <class T, bool GATED, int QB, RowEnd END>
-static void run_quantize(const QuantP& p, hipStream_t st) {
+static hipError_t run_quantize(const QuantP& p, hipStream_t st) {
   const int64_t strips = (p.rows + 15) / 16, nb = scale_blocks(p.cols);
-  k_quantize<T, GATED, QB, END><<<(unsigned)(strips * ((nb + QB - 1) / QB)), 256, 0, st>>>(p);
+  return launch(k_quantize<T, GATED, QB, END>, (unsigned)(strips * ((nb + QB - 1) / QB)), 256, p, st);
 }
 template <class T, RowEnd END>
-static void launch_quantize(const QuantP& p, bool weights, hipStream_t st) {
+static hipError_t launch_quantize(const QuantP& p, bool weights, hipStream_t st) {
   constexpr int QB = END == SHORT ? 1 : 4;
-  if (weights) k_quantize_block<T, END><<<(unsigned)(scale_blocks(p.rows) * scale_blocks(p.cols)), 256, 0, st>>>(p);
-  else if (p.gated) run_quantize<T, true, QB, END>(p, st);
-  else run_quantize<T, false, QB, END>(p, st);
+  if (weights) return launch(k_quantize_block<T, END>, (unsigned)(scale_blocks(p.rows) * scale_blocks(p.cols)), 256, p, st);
+  if (p.gated) return run_quantize<T, true, QB, END>(p, st);
+  return run_quantize<T, false, QB, END>(p, st);
 }
 template <class T>
-static void launch_quantize(const QuantP& p, bool weights, hipStream_t st) {
+static hipError_t launch_quantize(const QuantP& p, bool weights, hipStream_t st) {
   switch (row_end(p.cols)) {
     case WHOLE: return launch_quantize<T, WHOLE>(p, weights, st);
     case OVERLAP: return launch_quantize<T, OVERLAP>(p, weights, st);
-    case SHORT: return launch_quantize<T, SHORT>(p, weights, st);
+    default: return launch_quantize<T, SHORT>(p, weights, st);
   }
 }
 
@@ -127,7 +127,6 @@ extern "C" int svdmlp_quantize(const svdmlp_quantize_args* a, void* hip_stream) 
   if (a->rows == 0) return SVDMLP_OK;
   const QuantP p = {a->x, a->gated, (unsigned char*)a->codes, a->scales, a->x_ld, a->gated_ld, a->codes_ld, a->scales_ld,
                     a->rows, (int)a->cols};
-  if (a->type == SVDMLP_F32) launch_quantize<float>(p, weights, (hipStream_t)hip_stream);
-  else launch_quantize<__bf16>(p, weights, (hipStream_t)hip_stream);
-  return launch_status();
+  if (a->type == SVDMLP_F32) return status_of(launch_quantize<float>(p, weights, (hipStream_t)hip_stream));
+  return status_of(launch_quantize<__bf16>(p, weights, (hipStream_t)hip_stream));
 }

@@ -23,12 +23,18 @@ inline int check_codes(const void* codes, int64_t ld, int64_t cols) {
   if (!aligned_to(codes, 16) || ld % 16) return SVDMLP_INVALID_ARGUMENT;
   return ld < MAX_CODE_LD ? SVDMLP_OK : SVDMLP_UNSUPPORTED;
 }
-inline int launch_status() {
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? SVDMLP_OK : SVDMLP_HIP_ERROR;
-}
+inline int status_of(hipError_t e) { return e == hipSuccess ? SVDMLP_OK : SVDMLP_HIP_ERROR; }
 
 #ifdef __HIPCC__
+// One launch and its own error: the thread's last error may be one that an earlier call of the program left there.
+template <class P>
+hipError_t launch(void (*kernel)(P), unsigned workgroups, unsigned threads, const P& p, hipStream_t st) {
+  void* args[] = {const_cast<P*>(&p)};
+  const hipError_t e = hipLaunchKernel((const void*)kernel, dim3(workgroups), dim3(threads), args, 0, st);
+  if (e != hipSuccess) (void)hipGetLastError();      // reported by the status
+  return e;
+}
+
 // Eight consecutive elements of a row as they lie in memory, from any element's address (the hardware takes 16-byte
 // accesses at any alignment).
 template <class T>

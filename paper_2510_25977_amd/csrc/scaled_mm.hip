@@ -774,46 +774,44 @@ static int plan_mm(int64_t M, int64_t N, int64_t K, int out_type, int gated, MmP
 static size_t part_bytes(const MmPlan& q, int64_t M, int64_t N) { return q.join ? (size_t)q.ranges * M * N * 4 : 0; }
 
 template <RowEnd END>
-static void launch_join(const MmP& p, hipStream_t st) {
+static hipError_t launch_join(const MmP& p, hipStream_t st) {
   const unsigned wgs = (unsigned)((p.M + 15) / 16 * scale_blocks(p.N));
-  if (p.ranges == 1) k_mm_join<1, END><<<wgs, 256, 0, st>>>(p);
-  else if (p.ranges <= 4) k_mm_join<4, END><<<wgs, 256, 0, st>>>(p);
-  else if (p.ranges <= 8) k_mm_join<8, END><<<wgs, 256, 0, st>>>(p);
-  else k_mm_join<16, END><<<wgs, 256, 0, st>>>(p);
+  if (p.ranges == 1) return launch(k_mm_join<1, END>, wgs, 256, p, st);
+  if (p.ranges <= 4) return launch(k_mm_join<4, END>, wgs, 256, p, st);
+  if (p.ranges <= 8) return launch(k_mm_join<8, END>, wgs, 256, p, st);
+  return launch(k_mm_join<16, END>, wgs, 256, p, st);
 }
-static void launch_join(const MmP& p, hipStream_t st) {
+static hipError_t launch_join(const MmP& p, hipStream_t st) {
   switch (row_end(p.N)) {
     case WHOLE: return launch_join<WHOLE>(p, st);
     case OVERLAP: return launch_join<OVERLAP>(p, st);
-    case SHORT: return k_mm_join<4, SHORT><<<(unsigned)((p.M + 15) / 16), 256, 0, st>>>(p);
+    default: return launch(k_mm_join<4, SHORT>, (unsigned)((p.M + 15) / 16), 256, p, st);
   }
 }
 
 template <int MT>
-static void launch_tile(const MmP& p, unsigned wgs, hipStream_t st) {
-  if (p.part) k_mm_tile<MT, 4, 2, 4, true, false><<<wgs, 512, 0, st>>>(p);
-  else k_mm_tile<MT, 4, 2, 4, false, false><<<wgs, 512, 0, st>>>(p);
+static hipError_t launch_tile(const MmP& p, unsigned wgs, hipStream_t st) {
+  if (p.part) return launch(k_mm_tile<MT, 4, 2, 4, true, false>, wgs, 512, p, st);
+  return launch(k_mm_tile<MT, 4, 2, 4, false, false>, wgs, 512, p, st);
 }
-static void launch_mm(MmP& p, const MmPlan& q, bool gated, hipStream_t st) {
+static hipError_t launch_mm(MmP& p, const MmPlan& q, bool gated, hipStream_t st) {
   const unsigned wgs = (unsigned)(q.tiles * q.ranges);
   const MmKind& kind = MM_KIND[q.kind];
   const int mtiles = (p.M + kind.rows - 1) / kind.rows, ntiles = (p.N + kind.cols - 1) / kind.cols;
   p.tiles = (int)q.tiles;
   p.band = q.kind == MM_TILE_128_256 || q.kind == MM_TILE_256 ? band_height(mtiles, wgs) : p.M > p.N ? ntiles : mtiles;
   switch (q.kind) {
-    case MM_FEW: k_mm_few<<<wgs, 64 * FEW_WAVES, 0, st>>>(p); break;
-    case MM_RING_32: k_mm_ring<1, 2, false><<<wgs, 256, 0, st>>>(p); break;
-    case MM_RING_64: k_mm_ring<2, 2, false><<<wgs, 256, 0, st>>>(p); break;
+    case MM_FEW: return launch(k_mm_few, wgs, 64 * FEW_WAVES, p, st);
+    case MM_RING_32: return launch(k_mm_ring<1, 2, false>, wgs, 256, p, st);
+    case MM_RING_64: return launch(k_mm_ring<2, 2, false>, wgs, 256, p, st);
     case MM_RING_64_128:
-      if (gated) k_mm_ring<2, 4, true><<<wgs, 256, 0, st>>>(p);
-      else k_mm_ring<2, 4, false><<<wgs, 256, 0, st>>>(p);
-      break;
+      if (gated) return launch(k_mm_ring<2, 4, true>, wgs, 256, p, st);
+      return launch(k_mm_ring<2, 4, false>, wgs, 256, p, st);
     case MM_TILE_128_256:
-      if (gated) k_mm_tile<4, 4, 2, 4, false, true><<<wgs, 512, 0, st>>>(p);
-      else launch_tile<4>(p, wgs, st);
-      break;
-    case MM_RING_32_128: k_mm_ring<1, 4, true><<<wgs, 256, 0, st>>>(p); break;
-    default: launch_tile<8>(p, wgs, st); break;
+      if (gated) return launch(k_mm_tile<4, 4, 2, 4, false, true>, wgs, 512, p, st);
+      return launch_tile<4>(p, wgs, st);
+    case MM_RING_32_128: return launch(k_mm_ring<1, 4, true>, wgs, 256, p, st);
+    default: return launch_tile<8>(p, wgs, st);
   }
 }
 
@@ -866,9 +864,9 @@ int svdmlp_scaled_matmul(const svdmlp_scaled_matmul_args* a, void* hip_stream) {
   p.out_type = a->out_type;
   p.ranges = q.ranges; p.range_blocks = q.range_blocks;
   hipStream_t st = (hipStream_t)hip_stream;
-  launch_mm(p, q, a->gated != 0, st);
-  if (q.join) launch_join(p, st);
-  return launch_status();
+  hipError_t e = launch_mm(p, q, a->gated != 0, st);
+  if (e == hipSuccess && q.join) e = launch_join(p, st);
+  return status_of(e);
 }
 
 }  // extern "C"

@@ -3,6 +3,8 @@
 Tolerances count roundings: eps = 2^-23 for an fp32 operation (twice the half step, so that sums which the matrix cores round
 towards zero are covered), half a step for the rounding of a result: 2^-24 fp32, 2^-9 bf16 relative to a value's power of two
 (2^-8 relative to the value at most), e4m3 2^-4 relative, 2^-10 of its scale below its normal numbers."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -615,3 +617,31 @@ def test_a_block_made_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, expected)
+
+
+def hip_runtime():
+    """The HIP runtime that torch and the library have loaded."""
+    with open("/proc/self/maps") as f:
+        return ctypes.CDLL(next(line.split()[-1] for line in f if "libamdhip64" in line))
+
+
+def test_an_error_that_an_earlier_call_left_is_not_the_launchs():
+    """A call that failed before (here: a device that does not exist) leaves its error with the thread.  The operators launch what
+    they are asked for and report their own launches only."""
+    x = torch.randn(40, 256, device=dev()).to(BF16)
+    W = B.quantize(torch.randn(300, 256, device=dev()), block_rows=128)
+    A = B.quantize(x)
+    a16, w16 = B.quantize(torch.randn(16, 14336, device=dev())), B.quantize(torch.randn(512, 14336, device=dev()), block_rows=128)
+    calls = [lambda: B.quantize(x).scales, lambda: B.quantize(x, x).scales, lambda: B.quantize(x, block_rows=128).scales,
+             lambda: B.norm_in(x), lambda: B.norm_out(x, x, scaled=True)[1].scales, lambda: B.scaled_matmul(A, W),
+             lambda: B.scaled_matmul(A, W, gated=True), lambda: B.scaled_matmul(a16, w16, out_dtype=F8).scales]
+    want = [c() for c in calls]
+    torch.cuda.synchronize()
+    hip = hip_runtime()
+    for call, expected in zip(calls, want):
+        assert hip.hipSetDevice(1 << 20) != 0
+        try:
+            got = call()
+        finally:
+            hip.hipGetLastError()
+        assert torch.equal(got, expected)
