@@ -454,6 +454,8 @@ def _norm(x, branch, residual, weight, bias, kind, eps, weight_plus, residual_sc
     if isinstance(out, tuple):
         out = out if type(out) is Scaled else Scaled(*out)
         codes, scales = out
+    elif scaled:
+        raise ValueError("an 8-bit result goes to a Scaled, out is a plain tensor")
     else:
         codes, scales = out, None
     args = _tensors().norm_args(dev, branch, residual, weight, bias, kind, eps, weight_plus, residual_scale, branch_scale, gate,
@@ -526,6 +528,8 @@ def scaled_matmul(a, w, *, gated: bool = False, out=None, out_dtype: torch.dtype
     if isinstance(out, tuple):
         out = out if type(out) is Scaled else Scaled(*out)
         c, c_scales = out
+    elif out_dtype is _F8:
+        raise ValueError("an 8-bit result goes to a Scaled, out is a plain tensor")
     else:
         c, c_scales = out, None
     need = 0 if gated else svdmlp_scaled_matmul_workspace_bytes(M, N, K, SVDMLP_BF16 if c_scales is None else SVDMLP_F8)

@@ -206,6 +206,21 @@ def test_the_binding_checks_tensors(monkeypatch):
         B.SvdMlpF8(Ug=fake(256, 64), Vg=fake(65, 512), kind=B.SVDMLP_LINEAR)
 
 
+def test_a_plain_buffer_for_an_8_bit_result_is_refused(monkeypatch):
+    """A call that asks for codes and hands over a plain tensor would get the plain result without a word."""
+    monkeypatch.setattr(B, "_run", lambda *a: None)
+    x, plain = fake(4, 256), fake(4, 256)
+    a, w = B.empty_scaled(4, 256, "cpu"), B.empty_scaled(256, 256, "cpu", 128)
+    a = (a.codes.as_subclass(_OnDevice), a.scales)
+    codes = B.empty_scaled(4, 256, "cpu")
+    for call in (lambda out: B.norm_in(x, out=out, scaled=True), lambda out: B.norm_out(x, x.clone(), out=out, scaled=True)[1],
+                 lambda out: B.scaled_matmul(a, w, out=out, out_dtype=torch.float8_e4m3fn)):
+        with pytest.raises(ValueError, match="8-bit"):
+            call(plain)
+        assert call(codes) is codes and type(call(None)) is B.Scaled
+    assert B.scaled_matmul(a, w, out=codes) is codes and B.scaled_matmul(a, w, out=plain) is plain
+
+
 def fields_of(monkeypatch, call):
     """The argument structure that a call of the binding hands over, by field."""
     got = []
