@@ -266,7 +266,9 @@ int svdmlp_roof_empty_chain(int launches, int workgroups, int threads, void *hip
  * device, and a call only launches kernels on hip_stream (NULL = the default stream): no allocation, no synchronisation,
  * no memset, no copy, so it may be recorded into a HIP graph.  They return SVDMLP_OK, SVDMLP_INVALID_ARGUMENT,
  * SVDMLP_UNSUPPORTED, SVDMLP_WORKSPACE_TOO_SMALL or, if a launch fails, SVDMLP_HIP_ERROR.  Arguments are checked on the
- * host before anything is launched.  A call of no rows does nothing once its arguments are checked.
+ * host before anything is launched.  A call of no rows does nothing once its arguments are checked.  Outputs may not share a
+ * byte with an input or with each other (else SVDMLP_INVALID_ARGUMENT; what lies between rows does not count), but for
+ * svdmlp_norm's h in the place of its residual.
  *
  * 8-bit tensors ("scaled tensors").  SVDMLP_F8 names e4m3 codes (1 sign, 4 exponent, 3 mantissa bits, largest 448, no
  * infinities) that stand for code * scale.  Rows of codes start on 16 bytes (pointer and row stride are multiples of 16)
@@ -280,8 +282,7 @@ int svdmlp_roof_empty_chain(int launches, int workgroups, int threads, void *hip
 enum { SVDMLP_F8 = 2 };   /* a type of results and operands of the operators below; svdmlp_create does not take it */
 
 /* Quantise x, or SiLU(x) .* gated with `gated` (the hand-over between the gate / up products and the down projection).
- * rows < 2^24, cols <= 2^22, ceil(rows / 16) * ceil(cols / 128) < 2^23 (else SVDMLP_UNSUPPORTED).  Outputs must not overlap
- * inputs. */
+ * rows < 2^24, cols <= 2^22, ceil(rows / 16) * ceil(cols / 128) < 2^23 (else SVDMLP_UNSUPPORTED). */
 typedef struct {
   int64_t rows, cols;
   int32_t type;             /* of x and gated: SVDMLP_BF16 or SVDMLP_F32 */
@@ -307,7 +308,7 @@ enum { SVDMLP_GATE_PLAIN = 0, SVDMLP_GATE_SIGMOID = 1, SVDMLP_GATE_TANH = 2 };
  * AFTER a block is kind = RMS or LAYER; with next_kind it makes the norm before the next block of the same h.
  * Sums, h and both norms are fp32; the second norm takes h before it is rounded to its type.  A norm that is given no
  * weight or bias leaves it out; likewise branch_scale and gate.  Each row is read whole before any of it is written, so h
- * may be the residual's own buffer (same pointer and stride); otherwise outputs must not overlap inputs.
+ * may be the residual's own buffer (same pointer and stride).
  * d: 1 .. 32768, fewer than 2^25 rows up to d = 512, 2^24 up to 1024, 2^23 up to 2048, 2^22 up to 16384,
  * 2^21 beyond (else SVDMLP_UNSUPPORTED).  type / stream_type: BF16 / BF16, BF16 / F32 or F32 / F32. */
 typedef struct {
@@ -341,7 +342,7 @@ int svdmlp_norm(const svdmlp_norm_args *args, void *hip_stream);
  * eight consecutive codes have below 2^-13 of the power of two of the largest of them and are fp32 otherwise; the blocks'
  * sums are added in fp32.  M, N, K are free (1 <= N, K <= 2^22, M < 2^24, fewer than 2^22 tiles of 256 x 256, gated of
  * 128 x 256, else SVDMLP_UNSUPPORTED); where the contraction ends inside a block the rest of the block counts as zero whatever lies there.  The order of the sums depends on the extents alone: the same call
- * gives the same bits.  C must not overlap an operand.
+ * gives the same bits.
  * gated: the contraction is two in a row, K / 2 each and K a multiple of 256.  The first half's sums G and the second's P stay
  * fp32 and C = SiLU(G) .* P: the gate and up products of a block, whose operands lie side by side, in one call.
  * Some extents cut the contraction into ranges that different workgroups sum: their partial sums take

@@ -225,7 +225,7 @@ extern "C" int svdmlp_norm(const svdmlp_norm_args* a, void* hip_stream) {
   if ((a->kind == SVDMLP_NORM_NONE && (a->weight || a->bias)) || (!next && (a->next_weight || a->next_bias))) return SVDMLP_INVALID_ARGUMENT;
   if (a->gate && (a->gate_rows < 1 || a->gate_ld < a->d)) return SVDMLP_INVALID_ARGUMENT;
   if ((a->residual && a->residual_ld < a->d) || (a->branch && a->branch_ld < a->d) || (a->h && a->h_ld < a->d)) return SVDMLP_INVALID_ARGUMENT;
-  const size_t t = (size_t)type_bytes(a->type), s = (size_t)type_bytes(a->stream_type);
+  const int64_t t = type_bytes(a->type), s = type_bytes(a->stream_type), o = type_bytes(a->out_type);
   for (const void* q : {a->branch, a->weight, a->bias, a->branch_scale, a->gate, a->next_weight, a->next_bias})
     if (!aligned_to(q, t)) return SVDMLP_INVALID_ARGUMENT;
   if (!aligned_to(a->residual, s) || !aligned_to(a->h, s)) return SVDMLP_INVALID_ARGUMENT;
@@ -241,6 +241,13 @@ extern "C" int svdmlp_norm(const svdmlp_norm_args* a, void* hip_stream) {
   if (a->type == SVDMLP_F32 && a->stream_type == SVDMLP_BF16) return SVDMLP_UNSUPPORTED;
   if (a->d > 32768 || a->rows >= (int64_t(1) << 31) / row_threads(a->d)) return SVDMLP_UNSUPPORTED;   // registers; lanes of a grid
   if (a->rows == 0) return SVDMLP_OK;
+  auto vec = [&](const void* q) { return rows_of(q, 1, a->d, 0, t); };
+  if (outputs_overlap({rows_of(a->h, a->rows, a->d, a->h_ld, s), rows_of(a->out, a->rows, a->d, a->out_ld, o),
+                       activation_scales(next && o == 1 ? a->out_scales : nullptr, a->rows, a->d, a->out_scales_ld)},
+                      {rows_of(a->residual == a->h ? nullptr : a->residual, a->rows, a->d, a->residual_ld, s),
+                       rows_of(a->branch, a->rows, a->d, a->branch_ld, t), vec(a->weight), vec(a->bias), vec(a->branch_scale),
+                       rows_of(a->gate, a->gate ? (a->rows - 1) / a->gate_rows + 1 : 0, a->d, a->gate_ld, t), vec(a->next_weight), vec(a->next_bias)}))
+    return SVDMLP_INVALID_ARGUMENT;
   NormP p;
   p.residual = a->residual; p.branch = a->branch; p.weight = a->weight; p.bias = a->bias;
   p.branch_scale = a->branch_scale; p.gate = a->gate; p.next_weight = a->next_weight; p.next_bias = a->next_bias;

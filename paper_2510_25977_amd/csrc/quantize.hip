@@ -117,7 +117,7 @@ extern "C" int svdmlp_quantize(const svdmlp_quantize_args* a, void* hip_stream) 
   const bool weights = a->block_rows == SCALE_BLOCK;
   if (weights && a->gated) return SVDMLP_INVALID_ARGUMENT;
   if (!a->x || a->x_ld < a->cols || (a->gated && a->gated_ld < a->cols)) return SVDMLP_INVALID_ARGUMENT;
-  const size_t t = (size_t)type_bytes(a->type);
+  const int64_t t = type_bytes(a->type);
   if (!aligned_to(a->x, t) || !aligned_to(a->gated, t)) return SVDMLP_INVALID_ARGUMENT;
   if (const int st = check_codes(a->codes, a->codes_ld, a->cols)) return st;
   if (!a->scales || !aligned_to(a->scales, weights ? 4 : 2) || (!weights && a->scales_ld < a->rows)) return SVDMLP_INVALID_ARGUMENT;
@@ -125,6 +125,10 @@ extern "C" int svdmlp_quantize(const svdmlp_quantize_args* a, void* hip_stream) 
   if (a->rows >= int64_t(1) << 24 || a->cols > int64_t(1) << 22) return SVDMLP_UNSUPPORTED;
   if ((a->rows + 15) / 16 * scale_blocks(a->cols) >= int64_t(1) << 23) return SVDMLP_UNSUPPORTED;   // grid of 256 lanes below 2^31
   if (a->rows == 0) return SVDMLP_OK;
+  if (outputs_overlap({rows_of(a->codes, a->rows, a->cols, a->codes_ld, 1),
+                       weights ? weight_scales(a->scales, a->rows, a->cols) : activation_scales(a->scales, a->rows, a->cols, a->scales_ld)},
+                      {rows_of(a->x, a->rows, a->cols, a->x_ld, t), rows_of(a->gated, a->rows, a->cols, a->gated_ld, t)}))
+    return SVDMLP_INVALID_ARGUMENT;
   const QuantP p = {a->x, a->gated, (unsigned char*)a->codes, a->scales, a->x_ld, a->gated_ld, a->codes_ld, a->scales_ld,
                     a->rows, (int)a->cols};
   if (a->type == SVDMLP_F32) return status_of(launch_quantize<float>(p, weights, (hipStream_t)hip_stream));

@@ -2,6 +2,7 @@
 // reductions over lanes, and the host's argument checks.
 #pragma once
 #include "common.h"
+#include "rows.h"
 
 namespace svdmlp {
 
@@ -23,6 +24,11 @@ inline int check_codes(const void* codes, int64_t ld, int64_t cols) {
   if (!aligned_to(codes, 16) || ld % 16) return SVDMLP_INVALID_ARGUMENT;
   return ld < MAX_CODE_LD ? SVDMLP_OK : SVDMLP_UNSUPPORTED;
 }
+inline Rows rows_of(const void* at, int64_t rows, int64_t cols, int64_t ld, int64_t bytes) {
+  return Rows(at, rows, cols * bytes, rows > 1 ? ld * bytes : 0);
+}
+inline Rows activation_scales(const void* at, int64_t rows, int64_t cols, int64_t ld) { return rows_of(at, scale_blocks(cols), rows, ld, 2); }
+inline Rows weight_scales(const void* at, int64_t rows, int64_t cols) { return rows_of(at, 1, scale_blocks(rows) * scale_blocks(cols), 0, 4); }
 inline int status_of(hipError_t e) { return e == hipSuccess ? SVDMLP_OK : SVDMLP_HIP_ERROR; }
 
 #ifdef __HIPCC__

@@ -856,6 +856,12 @@ int svdmlp_scaled_matmul(const svdmlp_scaled_matmul_args* a, void* hip_stream) {
     if (a->workspace_bytes < part_bytes(q, a->M, a->N)) return SVDMLP_WORKSPACE_TOO_SMALL;
     if (!a->workspace || !aligned_to(a->workspace, 16)) return SVDMLP_INVALID_ARGUMENT;
   }
+  const bool f8 = a->out_type == SVDMLP_F8;
+  if (outputs_overlap({rows_of(a->c, a->M, a->N, a->c_ld, f8 ? 1 : 2), activation_scales(f8 ? a->c_scales : nullptr, a->M, a->N, a->c_scales_ld),
+                       rows_of(q.join ? a->workspace : nullptr, 1, (int64_t)part_bytes(q, a->M, a->N), 0, 1)},
+                      {rows_of(a->a, a->M, a->K, a->a_ld, 1), activation_scales(a->a_scales, a->M, a->K, a->a_scales_ld),
+                       rows_of(a->w, a->N, a->K, a->w_ld, 1), weight_scales(a->w_scales, a->N, a->K)}))
+    return SVDMLP_INVALID_ARGUMENT;
   MmP p;
   p.a = (const char*)a->a; p.w = (const char*)a->w; p.sa = (const __bf16*)a->a_scales; p.sw = a->w_scales;
   p.c = a->c; p.c_scales = (__bf16*)a->c_scales; p.part = q.join ? (float*)a->workspace : nullptr;

@@ -645,3 +645,37 @@ def test_an_error_that_an_earlier_call_left_is_not_the_launchs():
         finally:
             hip.hipGetLastError()
         assert torch.equal(got, expected)
+
+
+def test_operands_side_by_side_in_one_buffer():
+    """Column ranges of one buffer, results beside inputs: no byte is shared, so the calls run, with the bits of calls on
+    buffers of their own."""
+    M, d, N = 70, 256, 128
+    r = rng(15)
+    whole = torch.zeros(M, 8 * d, dtype=torch.uint8, device=dev())
+    x = whole[:, :2 * d].view(BF16)
+    y = whole[:, 2 * d:4 * d].view(BF16)
+    h = whole[:, 4 * d:6 * d].view(BF16)
+    codes = whole[:, 6 * d:7 * d].view(F8)
+    c = whole[:, 7 * d:].view(BF16)                  # [M, N]
+    for t in (x, y):
+        t.copy_(torch.from_numpy(r.normal(size=(M, d))))
+    w = torch.from_numpy(r.normal(size=d)).to(BF16).to(dev())
+    W = B.quantize(torch.from_numpy(r.normal(size=(N, d))).to(BF16).to(dev()), block_rows=128)
+    scales = torch.empty(2, M, dtype=BF16, device=dev())
+    x0, y0 = x.clone(), y.clone()
+    B.quantize(x, y, out=(codes, scales))
+    want = B.quantize(x0, y0)
+    assert torch.equal(codes.contiguous().view(torch.uint8), want.codes.view(torch.uint8)) and torch.equal(scales, want.scales)
+    B.norm_out(y, x, w, h=h, next_weight=w, out=(codes, scales))
+    want_h, want = B.norm_out(y0, x0, w, next_weight=w, scaled=True)
+    assert torch.equal(h, want_h) and torch.equal(codes.contiguous().view(torch.uint8), want.codes.view(torch.uint8))
+    B.scaled_matmul((codes, scales), W, out=c)
+    assert torch.equal(c, B.scaled_matmul(want, W))
+    assert torch.equal(x, x0) and torch.equal(y, y0) and torch.equal(h, want_h)
+    # shifted by a row, results would lie on inputs that other workgroups have yet to read
+    with pytest.raises(B.SvdMlpError):
+        B.norm_out(y[:-1], x[:-1], w, h=x[1:])
+    with pytest.raises(B.SvdMlpError):
+        B.quantize(x[:-1], out=(whole[1:, :d].view(F8), scales[:, 1:]))
+    assert torch.equal(x, x0)

@@ -2,6 +2,7 @@
 import ctypes
 import re
 import struct
+import subprocess
 import types
 
 import numpy as np
@@ -33,6 +34,67 @@ def status(name, **changed):
     fields, layout = CALLS[name]
     assert set(changed) <= set(fields)
     return getattr(B.lib(), name)(layout.pack(*{**fields, **changed}.values()), None)
+
+
+def test_overlap_of_matrices_byte_for_byte(tmp_path):
+    """The host's check for shared memory against sets of bytes, over all small matrices of a buffer: no overlap is missed and
+    none is seen where rows of one lie in the gaps of the other."""
+    (tmp_path / "t.cpp").write_text(r"""
+#include <cstdio>
+#include "rows.h"
+using namespace svdmlp;
+int main() {
+  static char buf[1];
+  const int64_t base = (int64_t)(uintptr_t)buf;      // addresses only, nothing is read
+  long cases = 0, wrong = 0, shared = 0;
+  auto at = [&](int64_t x) { return (const void*)(uintptr_t)(base + x); };
+  for (int ra = 1; ra <= 4; ++ra) for (int wa = 1; wa <= 4; ++wa) for (int la = wa; la <= 7; ++la)
+  for (int rb = 1; rb <= 4; ++rb) for (int wb = 1; wb <= 4; ++wb) for (int lb = wb; lb <= 7; ++lb)
+  for (int off = 0; off < 30; ++off) {
+    unsigned long long a = 0, b = 0;
+    for (int r = 0; r < ra; ++r) for (int e = 0; e < wa; ++e) a |= 1ull << (r * la + e);
+    for (int r = 0; r < rb; ++r) for (int e = 0; e < wb; ++e) b |= 1ull << (off + r * lb + e);
+    const Rows x{at(0), ra, wa, la}, y{at(off), rb, wb, lb};
+    const bool want = a & b;
+    wrong += overlap(x, y) != want;
+    wrong += overlap(y, x) != want;
+    shared += want;
+    ++cases;
+  }
+  wrong += overlap({at(0), 1, 4, 0}, {at(4), 1, 4, -9}) + !overlap({at(0), 1, 4, 0}, {at(3), 1, 4, 0});      // one row: no stride
+  wrong += overlap({nullptr, 4, 4, 4}, {at(0), 4, 4, 4}) + overlap({at(0), 0, 4, 4}, {at(0), 4, 4, 4});
+  std::printf("%ld %ld %ld", cases, shared, wrong);
+}
+""")
+    subprocess.run(["g++", "-std=c++17", "-O1", f"-I{ROOT}/paper_2510_25977_amd/csrc", "t.cpp", "-o", "t"], cwd=tmp_path, check=True)
+    cases, shared, wrong = map(int, subprocess.run([str(tmp_path / "t")], capture_output=True, text=True, check=True).stdout.split())
+    assert wrong == 0 and 0 < shared < cases == 30 * (4 * (7 + 6 + 5 + 4)) ** 2
+
+
+@pytest.mark.parametrize("name,changed", [
+    # rows of 512 bytes of x, 256 of codes; each call shares memory between what it writes and something else
+    ("svdmlp_quantize", dict(codes=0x1100)), ("svdmlp_quantize", dict(codes=0xF00)), ("svdmlp_quantize", dict(scales=0x1700)),
+    ("svdmlp_quantize", dict(gated=0x8000, gated_ld=256, codes=0x8010)), ("svdmlp_quantize", dict(scales=0x2100)),
+    ("svdmlp_quantize", dict(block_rows=128, scales=0x17FC)),
+    ("svdmlp_norm", dict(h=0x1200)), ("svdmlp_norm", dict(h=0xE00)), ("svdmlp_norm", dict(h=0x2004)), ("svdmlp_norm", dict(h=0x2E02)),
+    ("svdmlp_norm", dict(h=0x41FE)), ("svdmlp_norm", dict(out=0x1100)), ("svdmlp_norm", dict(out=0x2700)), ("svdmlp_norm", dict(out=0x5100)),
+    ("svdmlp_norm", dict(out_scales=0x30FE)), ("svdmlp_norm", dict(out_scales=0x6080)), ("svdmlp_norm", dict(out_scales=0x5100)),
+    ("svdmlp_norm", dict(out_type=BF16, out=0x6000, h=0x6100)), ("svdmlp_norm", dict(bias=0x5010)), ("svdmlp_norm", dict(next_bias=0x6010)),
+    ("svdmlp_scaled_matmul", dict(c=0x1100)), ("svdmlp_scaled_matmul", dict(c=0x10010)), ("svdmlp_scaled_matmul", dict(c=0x2080)),
+    ("svdmlp_scaled_matmul", dict(c=0x20000)), ("svdmlp_scaled_matmul", dict(c_scales=0x50C0)), ("svdmlp_scaled_matmul", dict(c_scales=0x10100)),
+])
+def test_outputs_that_share_memory_are_refused(name, changed):
+    matmul = name == "svdmlp_scaled_matmul"
+    four = dict(M=4, w=0x10000, w_scales=0x20000) if matmul else dict(rows=4)       # all apart but for what is changed
+    assert status(name, **four, **changed) == BAD
+
+
+@pytest.mark.parametrize("workspace", [0x1000010, 0x1100000, 0x2000000, 0x2800000, 0x3000000 - 16, 0x3100000])
+def test_a_workspace_that_shares_memory_is_refused(workspace):
+    args = dict(M=16, N=512, K=14336, a=0x1000000, a_ld=14336, a_scales=0x1100000, w=0x2000000, w_ld=14336, w_scales=0x2800000,
+                c=0x3000000, c_ld=512, c_scales=0x3100000, workspace=workspace)
+    assert B.svdmlp_scaled_matmul_workspace_bytes(16, 512, 14336, F8) > 16
+    assert status("svdmlp_scaled_matmul", **args) == BAD
 
 
 def test_packed_arguments_are_the_headers_structures():
