@@ -277,7 +277,10 @@ int svdmlp_roof_empty_chain(int launches, int workgroups, int threads, void *hip
  *                       is scales[b * scales_ld + m], scales_ld >= R (a product reads the scales of 256 rows at a time)
  *   weights [N, K]    : one fp32 scale per 128 x 128: scales[(n / 128) * ceil(K / 128) + k / 128]
  * What is quantised here has scale = max(largest magnitude of the block / 448, 2^-100), for activations rounded to bf16, and
- * codes v / scale rounded to nearest even, both up to one rounding in fp32 before that.  A NaN gets the NaN code; a block that
+ * codes v / scale rounded to nearest even.  Either quotient is a product with the reciprocal, both rounded to nearest in fp32:
+ * two roundings before the last, so what lies that near to a border may get the neighbouring code or bf16 scale.  v is x
+ * itself, SiLU(x) .* gated in fp32 (relative to |x| + 8 times 2^-23: exp takes a rounded argument), or the fp32 value of the
+ * norm or product that makes the 8-bit result.  A NaN gets the NaN code and leaves its block's scale alone; a block that
  * holds an infinity gets the scale infinity and stands for NaN throughout. */
 enum { SVDMLP_F8 = 2 };   /* a type of results and operands of the operators below; svdmlp_create does not take it */
 

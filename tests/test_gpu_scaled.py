@@ -679,3 +679,28 @@ def test_operands_side_by_side_in_one_buffer():
     with pytest.raises(B.SvdMlpError):
         B.quantize(x[:-1], out=(whole[1:, :d].view(F8), scales[:, 1:]))
     assert torch.equal(x, x0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_where_the_quantiser_rounds(dtype):
+    """Bit for bit: the scale is the largest magnitude times 1 / 448, the code that of v times 1 / scale, each reciprocal rounded to
+    fp32 before its product is.  (Torch on the CPU in fp32, which rounds every operation to nearest even.)"""
+    r = rng(16)
+    x = torch.from_numpy(r.normal(size=(300, 700)) * np.exp(4 * r.normal(size=(300, 1)))).to(dtype)
+    x[7], x[8, :128] = 0, torch.finfo(dtype).tiny
+    v = torch.nn.functional.pad(x.float(), (0, 68)).view(300, 6, 128)
+    smallest, inv448 = torch.tensor(2.0 ** -100), torch.tensor(1.0) / 448
+    for block_rows in (1, 128):
+        got = B.quantize(x.to(dev()), block_rows=block_rows)
+        amax = v.abs().amax(2)
+        if block_rows == 1:
+            s = torch.maximum(amax * inv448, smallest).to(BF16)
+            assert torch.equal(got.scales.cpu(), s.t())
+            s = s.float()
+        else:
+            amax = torch.nn.functional.pad(amax, (0, 0, 0, 84)).view(3, 128, 6).amax(1)
+            s = torch.maximum(amax * inv448, smallest)
+            assert torch.equal(got.scales.cpu(), s)
+            s = s.repeat_interleave(128, 0)[:300]
+        q = (v * (1.0 / s)[:, :, None]).clamp(-448, 448).to(F8).view(300, 768)[:, :700]
+        assert np.array_equal(bytes_of(got.codes), bytes_of(q))
