@@ -342,6 +342,7 @@ class SvdMlp:
 
 
 # ---- operators around a factored layer in 8 bits -----------------------------------------------------------------------
+# Forward only, as the rest of the binding: results carry no gradient, whatever their inputs require.
 class Scaled(NamedTuple):
     """An 8-bit tensor: codes [R, C] (torch.float8_e4m3fn, rows starting on 16 bytes) times scales: activations bfloat16
     [ceil(C / 128), R], one per row and 128 columns; weights float32 [ceil(R / 128), ceil(C / 128)], one per 128 x 128."""
@@ -541,7 +542,13 @@ def scaled_matmul(a, w, *, gated: bool = False, out=None, out_dtype: torch.dtype
 
 class SvdMlpF8:
     """``SvdMlp`` in 8 bits: the factors are quantised once (a scale per 128 x 128), activations between the products carry a
-    scale per row and 128 columns, the result is bfloat16.  Arguments as ``SvdMlp``; no context, no limit on the row count."""
+    scale per row and 128 columns, the result is bfloat16.  ``kind`` and the factors are ``SvdMlp``'s (any strides; not needed
+    afterwards); there is no context, no flags and no max_M: rows as many as the operators take.  On another stream than that of
+    its construction the block may be called at once; it has to live until what it was called for there is done.
+
+    Half the weight bytes for an error of about 0.09 of the result in the root mean square.  Faster than ``SvdMlp`` from about 100
+    rows on, not below (4096 x 14336, rank 512, from codes, in a graph: 21.5 us, bfloat16 20.1, at one row; 46.7, 63.1 at 512; 183,
+    234 at 4096); and slow at few rows where ffn is small beside the rank, since the gated product does not cut its contraction."""
 
     def __init__(self, *, Ug: torch.Tensor, Vg: torch.Tensor, Uu: Optional[torch.Tensor] = None, Vu: Optional[torch.Tensor] = None,
                  Ud: Optional[torch.Tensor] = None, Vd: Optional[torch.Tensor] = None, kind: int = SVDMLP_GATED):

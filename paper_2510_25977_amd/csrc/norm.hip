@@ -1,8 +1,9 @@
 // The norms around a block of the residual stream, with the residual, the gate and the scales, in one pass:
 //   b = [norm(branch) (weight + plus) + bias] branch_scale act(gate)    h = residual_scale residual + b    out = norm(h) ..
 // A row lies in the registers of its threads in fp32 from its first load to its last store, so every input is read once and
-// every result written once, and HBM bounds it: 4096 x 4096 with a residual into 8 bits 117 MB in 25.4 us (4.6 TB/s; a copy of
-// 2 GiB moves 4.8), 8192 x 5120 with an fp32 residual 503 MB in 91 us (5.5 TB/s), with a tanh gate and scale 109 us.
+// every result written once, and HBM bounds it (in a graph, over as many sets of tensors as no cache holds): 4096 x 4096 with a
+// residual into 8 bits 118 MB in 24.9 us (4.7 TB/s; a copy of 2 GiB moves 4.8), 8192 x 5120 with an fp32 residual 503 MB in 91 us
+// (5.5 TB/s), with a tanh gate and scale 108 us.
 #include "scaled.h"
 
 namespace svdmlp {
@@ -72,9 +73,10 @@ __device__ __forceinline__ float activated(float g, int act) {
 }
 
 // TPR threads hold a row, thread t columns 8 (i TPR + t) .. + 7, i < NV: 16 lanes hold a block of 128 columns.  Weights come with the
-// row up to two vectors a thread (4096 x 4096 26.3 us, 30.6 after the row's sum), with four they come when they are needed: the
-// registers allow half the waves otherwise (2048 x 16384 with gate and fp32 residual 102 us, 121; 2048 x 32768 fp32 136, 295).  At
-// one vector of bf16 the biases, the scale and the gate come along too (3616 x 3968 with all of them 33.0 us, 35.5 later).
+// row up to two vectors a thread (4096 x 4096 24.9 us, 25.4 after the row's sum), with four they come when they are needed: the
+// registers allow half the waves otherwise (2048 x 16384 with every input and an fp32 residual 120 us, 143; fp32 RMS norm of 2048 x
+// 32768 123, 237).  At one vector of bf16 the biases, the scale and the gate come along too (3616 x 3968 with all of them 32.7 us,
+// 35.0 later).
 template <class T, class S, int TPR, int NV, RowEnd END>
 __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void k_norm(NormP p) {
   constexpr int WAVES = TPR / 64;
@@ -186,9 +188,9 @@ static hipError_t run_norm(const NormP& p, hipStream_t st) {
 }
 
 // As few vectors a thread as a workgroup's size allows: a row's chain (loads, sums over the workgroup, stores) is what a CU has
-// four of at 512 threads.  us in a graph, 1024 / 512 / 256 / 128 threads for the row: 4096 x 4096 in 8 bits with a residual
-// 27.6 / 26.3 / 26.3 / 28.5, one such row 5.0 / 4.6 / 4.9, 8192 x 5120 with gate and fp32 residual - / 109 / 113 / 139;
-// 5359 x 562 with all inputs 11.9 with 128 threads, 16.1 with 256.
+// four of at 512 threads.  us in a graph over several sets, 1024 / 512 / 256 / 128 threads for the row: 4096 x 4096 in 8 bits with
+// a residual 26.4 / 24.9 / 25.6 / 29.3, one such row 3.1 / 2.8 / 3.4 / 4.6, 8192 x 5120 with every input and an fp32 residual 166 /
+// 120 / 126 / -; 5359 x 562 with all inputs 13.4 with 128 threads, 16.8 with 256.
 static int row_threads(int64_t d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 16384 ? 512 : 1024; }
 
 template <class T, class S>

@@ -1,6 +1,7 @@
 // Quantiser to e4m3 codes with a scale per block: scale = max(amax / 448, 2^-100), code = nearest even of v / scale.
 // Bounded by HBM: 2 (gated 4) bytes of bf16 read and one written per element, about twenty vector instructions on it;
-// 4096 x 14336 gated 294 MB in 56 us (5.2 TB/s; a copy of 2 GiB moves 4.8), not gated 177 MB in 33 us.
+// 4096 x 14336 gated 294 MB in 56 us (5.2 TB/s; a copy of 2 GiB moves 4.8), not gated 177 MB in 34 us (in a graph, over as many
+// sets of tensors as no cache holds); weights of 28672 x 4096, once, 353 MB in 65 us (by the profiler).
 #include "scaled.h"
 
 namespace svdmlp {
@@ -84,8 +85,10 @@ __global__ __launch_bounds__(256) void k_quantize_block(QuantP p) {
   if (threadIdx.x == 0) ((float*)p.scales)[blockIdx.x] = s;
 }
 
-// 1 / 2 / 4 blocks a group take, in a graph, 66.8 / 63.6 / 59.0 us at 4096 x 14336 gated, 6.0 / 5.6 / 5.2 us at 16 x 14336; with
-// four, 1777 x 7301 gated takes 15.1 us (4.3 TB/s), 1777 x 7304 14.4.  Rows of less than eight columns have one block.
+// Blocks a group: 1 / 2 / 4 take, in a graph over several sets, 53.2 / 54.4 / 56.0 us at 4096 x 14336 gated, 34.1 / 32.2 / 33.7 not
+// gated, 13.0 / 12.2 / 12.4 at 4096 x 4096, 17.7 / 17.0 / 17.9 at 1777 x 7301 gated: within 5 %.  At few rows, where workgroups are
+// few, four are the slowest: 2.4 / 2.7 / 3.4 us at 16 x 14336 gated, of the 4.2 us that a call takes the host.  Rows of less than
+// eight columns have one block.
 template <class T, bool GATED, int QB, RowEnd END>
 static hipError_t run_quantize(const QuantP& p, hipStream_t st) {
   const int64_t strips = (p.rows + 15) / 16, nb = scale_blocks(p.cols);

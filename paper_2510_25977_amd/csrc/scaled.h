@@ -62,7 +62,7 @@ struct Raw8<float> {
 // How rows of n columns end, for kernels whose lanes hold eight consecutive columns each, from a multiple of 8 on.  WHOLE: n is a
 // multiple of 8.  OVERLAP: the last vector that begins inside is read from column n - 8 on, and its first columns, which the lane
 // before it has too, are left out of sums and stores; so no lane loads element by element, and waits for that, while the others
-// wait for it at the row's next barrier (fp32 RMS norm of 4096 x 4091: 37 us; 4096 x 4096 takes 27.4).  SHORT: rows
+// wait for it at the row's next barrier (fp32 RMS norm of 4096 x 4091: 37 us that way, 28.7 this; 4096 x 4096 27.0).  SHORT: rows
 // of less than eight columns, element by element.
 enum RowEnd { WHOLE, OVERLAP, SHORT };
 inline RowEnd row_end(int64_t n) { return n % 8 == 0 ? WHOLE : n > 8 ? OVERLAP : SHORT; }

@@ -300,13 +300,21 @@ __device__ __forceinline__ void wait_copies(int t, int steps) {
 // of step t - 1 in phase 2 t - 1).  Before a step it waits for its A, in the middle of one for its share of the next W,
 // which the first half reads in the next phase.
 //
-// Bound by the matrix cores at the clock that they hold under power: 4096 x 8192 x 16384 (rows, contraction, columns) takes
-// 445 us = 2.47 PFLOP/s, the same on zeros 364 us (3.0 PFLOP/s); in step, without the half step between them, 486 us.  4096 x 4096 x
-// 4096, one tile a CU, takes 60 us = 2.29 PFLOP/s: a tile's first copies and its result, 5 us, stand alone there.
+// That is what the order needs; what is waited for is more.  The scales of step t + 1 are loads into registers, for which the
+// compiler waits at the end of step t with vmcnt(0), since it does not count the copies issued after them: A of step t + 1 and W of
+// step t + 2 have landed by then too, so a copy of W has one step to do so, not one and a half.  Where the matrix ends inside a
+// lane's MT rows those loads are single ones, waited for before the step's copies are issued (1777 and 1776 rows x 2687 x 7301:
+// 40.9 and 40.5 us).
+//
+// 4096 x 8192 x 16384 (rows, contraction, columns) takes 416-450 us by the card (2.4-2.6 PFLOP/s), the same on zeros 336-364; in
+// step, without the half step between them, 486 us.  Its matrix units work in 0.68 of a busy CU's clocks: what bounds it are the
+// waits of a step and the clock that power leaves.  4096 x 4096 x 4096, one tile a CU, takes 60 us = 2.29 PFLOP/s: a tile's first
+// copies and its result, 5 us, stand alone there.
 // PARTS: the workgroup sums a range of the contraction, where tiles are fewer than CUs and the contraction is long.
 // GATED: the sums of the contraction's first half wait in registers while the second half is summed, then SiLU(first) second is
-// the result: 4096 x (512 + 512) x 14336 into 8 bits 96-107 us, where two products into bf16 and the gated quantiser took 133 (in a
-// graph; 117 MB each that are not written and read).  The 256 x 256 tile has no registers for two sums, the smaller ones of
+// the result: 4096 x (512 + 512) x 14336 into 8 bits 97-107 us, where two products into bf16 and the gated quantiser take 153 (in a
+// graph; 117 MB each that are not written and read), 128 rows 9.9 and 16.4, one 7.0 and 10.3.  Its contraction is not cut, so a
+// narrow result of a long one leaves most CUs without work at few rows: 16 x (4096 + 4096) x 1400 31 us, those three 16.  The 256 x 256 tile has no registers for two sums, the smaller ones of
 // k_mm_ring not the 128 columns of a scale.
 template <int MT, int NT, int WM, int WN>
 struct MmTile {
@@ -696,7 +704,7 @@ __global__ __launch_bounds__(256) void k_mm_join(MmP p) {
 //   4096 x 4096 x 4096  tile 256x256 59.1 / 60.0, tile 128x256 69.8 / 72.9
 //   4096 x 8192 x 16384 tile 256x256 434 / 446, tile 128x256 540 / 560
 //   286 x 13184 x 7424  tile 256x256 in 4 ranges 62 / 58, in one 148 / 143
-//   4096 x 14336 x 512  ring 64x64 45 / 50, tile 128x256 in 4 ranges 50 / 44, in one 105 / 93
+//   4096 x 14336 x 512  ring 64x64 45 / 50, tile 128x256 in 4 ranges 50 / 44, in one 105 / 93 (the model misses the fastest here)
 // Gated, into 8 bits: 1 x 1024 x 14336  ring 32x128 7.3 / 7.4, ring 64x128 9.4 / 9.6;  512 x 1024 x 14336  tile 128x256 15.5 / 16.4, ring
 // 64x128 26 / 22;  4096 x 1024 x 14336  tile 128x256 93 / 96, ring 64x128 167 / 129.
 // (Further tiles measured and not kept: 128 x 128 with four waves, 256 x 128, 128 x 64: level or behind one of these.)
