@@ -704,3 +704,24 @@ def test_where_the_quantiser_rounds(dtype):
             s = s.repeat_interleave(128, 0)[:300]
         q = (v * (1.0 / s)[:, :, None]).clamp(-448, 448).to(F8).view(300, 768)[:, :700]
         assert np.array_equal(bytes_of(got.codes), bytes_of(q))
+
+
+def test_a_block_of_strided_factors_that_require_a_gradient():
+    """Factors of any strides, parameters among them, give the bits of contiguous ones; results carry no gradient."""
+    r = rng(17)
+    f = make_block(r, 512, 776, 128, 136)
+    x = torch.from_numpy(r.normal(size=(20, 512))).to(BF16).to(dev())
+    want = B.SvdMlpF8(**f)(x)
+    strided = {}
+    for i, (k, v) in enumerate(f.items()):
+        if i % 2:
+            strided[k] = torch.nn.Parameter(v.t().contiguous()).t()            # columns in one piece
+        else:
+            wide = torch.zeros(v.shape[0], v.shape[1] + 24, dtype=BF16, device=dev())
+            wide[:, 8:8 + v.shape[1]] = v
+            strided[k] = torch.nn.Parameter(wide)[:, 8:8 + v.shape[1]]
+    got = B.SvdMlpF8(**strided)(x.clone().requires_grad_())
+    assert torch.equal(got, want) and not got.requires_grad
+    U, V = strided["Ug"], strided["Vg"]
+    lin = B.SvdMlpF8(Ug=U, Vg=V, kind=B.SVDMLP_LINEAR)
+    assert torch.equal(lin(x), B.SvdMlpF8(Ug=f["Ug"], Vg=f["Vg"], kind=B.SVDMLP_LINEAR)(x))
